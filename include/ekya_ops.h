@@ -5,7 +5,8 @@
  * built from (the layers of the ResNet18 edge classifier of section 6.1 and
  * the PyTorch training the paper runs, section 5), so that each kernel can be
  * compared with an independent implementation.  They are synchronous: each
- * call enqueues on `stream`, waits for it, and frees its temporaries.
+ * call enqueues on `stream`, waits for it, and frees its temporaries.  (The
+ * adapter-training operators at the end are not: see there.)
  *
  * Common rules: every tensor pointer is a device pointer owned by the caller;
  * activations are NHWC with element type per `precision` (EKYA_FP32 float,
@@ -97,6 +98,53 @@ ekya_status ekya_op_sgd(float* w, float* v, const float* g, long long n, float l
  * frames [n,H,W,3] to [n,r,r,3]. */
 ekya_status ekya_op_resize(int precision, const void* frames, int n, int H, int W, int r,
                            void* out, void* stream);
+
+/* ------------------------------------------------- adapter-training operators
+ * What fine-tuning an adapter or a head on the network's features needs beside
+ * the layers above: group norm in place of BatchNorm (whose batch statistics
+ * say little on a few frames).
+ *
+ * These calls are asynchronous: they queue kernels on `stream` (of the current
+ * device), allocate nothing, copy nothing and never wait, so they can be
+ * captured into a HIP graph.  Scratch memory is the caller's: `workspace`, at
+ * least as many bytes as the matching *_workspace query says (host only, 0 if
+ * an argument is invalid), on 16 bytes, written before it is read, free for
+ * other use once the call's work has run; calls that may overlap on the GPU,
+ * and graphs that may, need one each.  Types per `precision` as above; any
+ * channel count, size and alignment to the element is accepted.  Results do
+ * not depend on other work on the GPU: every sum has a fixed order. */
+typedef enum {
+  EKYA_ACT_NONE = 0,
+  EKYA_ACT_RELU = 1, /* max(u, 0); derivative 0 at 0 */
+  EKYA_ACT_SILU = 2, /* u / (1 + exp(-u)) */
+  EKYA_ACT_GELU = 3  /* u (1 + erf(u / sqrt 2)) / 2 */
+} ekya_act;
+
+/* Group norm of x[N, HW, C], channels last: the C channels form `groups`
+ * groups of C / groups consecutive ones, and each (sample, group) is
+ * normalised by its own mean and biased variance over HW * C / groups
+ * elements: u = (x - mean) * rstd * gamma + beta, rstd = 1 / sqrt(var + eps),
+ * y = act(u).  gamma and beta [C] fp32, both or neither (null: 1 and 0).
+ * mean, rstd: [N, groups] fp32 outputs, read by the backward pass.  y may be x
+ * and overlaps it in no other way.  N >= 0 (0: nothing is done), HW >= 1, C in
+ * [1, 65536], N * HW * C <= 2^40, eps > 0. */
+size_t ekya_op_groupnorm_workspace(int precision, int N, long long HW, int C, int groups);
+ekya_status ekya_op_groupnorm(int precision, const void* x, int N, long long HW, int C, int groups,
+                              const float* gamma, const float* beta, float eps, int act, void* y,
+                              float* mean, float* rstd, void* workspace, size_t workspace_bytes,
+                              void* stream);
+/* Its gradient: with g = dy * act'(u), dbeta = sum g and dgamma = sum g * xhat
+ * over samples and pixels, h = g * gamma and dx = rstd * (h - avg(h) -
+ * xhat * avg(h * xhat)), averages over the (sample, group).  dgamma and dbeta
+ * [C] fp32, both or neither; N = 0 makes them zero.  dx may be dy or x, and
+ * overlaps them in no other way.  gamma, beta, mean and rstd as the forward
+ * call had and returned them. */
+size_t ekya_op_groupnorm_backward_workspace(int precision, int N, long long HW, int C, int groups);
+ekya_status ekya_op_groupnorm_backward(int precision, const void* dy, const void* x, int N,
+                                       long long HW, int C, int groups, const float* gamma,
+                                       const float* beta, const float* mean, const float* rstd,
+                                       int act, void* dx, float* dgamma, float* dbeta,
+                                       void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

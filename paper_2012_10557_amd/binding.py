@@ -25,6 +25,10 @@ EKYA_ERR_UNSUPPORTED = 5
 EKYA_FP32 = 0
 EKYA_BF16 = 1
 EKYA_MAX_EPOCHS = 64
+EKYA_ACT_NONE = 0
+EKYA_ACT_RELU = 1
+EKYA_ACT_SILU = 2
+EKYA_ACT_GELU = 3
 
 
 class EkyaError(RuntimeError):
@@ -164,6 +168,12 @@ _SIGS = {
     "ekya_op_softmax_ce": (_I, [_P, _P, _I, _I, _P, _P, _P]),
     "ekya_op_sgd": (_I, [_P, _P, _P, _LL, _F, _F, _P]),
     "ekya_op_resize": (_I, [_I, _P, _I, _I, _I, _I, _P, _P]),
+    "ekya_op_groupnorm_workspace": (ctypes.c_size_t, [_I, _I, _LL, _I, _I]),
+    "ekya_op_groupnorm": (_I, [_I, _P, _I, _LL, _I, _I, _P, _P, _F, _I, _P, _P, _P, _P,
+                               ctypes.c_size_t, _P]),
+    "ekya_op_groupnorm_backward_workspace": (ctypes.c_size_t, [_I, _I, _LL, _I, _I]),
+    "ekya_op_groupnorm_backward": (_I, [_I, _P, _P, _I, _LL, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P,
+                                        _P, ctypes.c_size_t, _P]),
 }
 
 _lib: Optional[ctypes.CDLL] = None
@@ -680,6 +690,82 @@ def ekya_op_resize(frames, r: int):
     out = torch.empty(n, r, r, 3, dtype=frames.dtype, device=frames.device)
     _op(load().ekya_op_resize(_precision(frames), _dev(frames), n, H, W, r, _dev(out), _stream()))
     return out
+
+
+# ----------------------------------------------- adapter-training operators
+# Asynchronous on the current stream.  Scratch comes from torch's allocator,
+# which hands it out again in that stream's order; a graph's own calls draw on
+# the graph's pool.
+def _on_current(x, *others):
+    """x's device must be the current one, and the other tensors' (None: absent)."""
+    torch = _torch()
+    if not x.is_cuda or x.device.index != torch.cuda.current_device():
+        raise ValueError("tensors must live on the current GPU")
+    for t in others:
+        if t is not None and t.device != x.device:
+            raise ValueError("tensors must live on one GPU")
+
+
+def _scratch(nbytes: int, device):
+    return _torch().empty(nbytes, dtype=_torch().uint8, device=device) if nbytes else None
+
+
+def _shaped(t, shape, name: str):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
+    return t
+
+
+def _groupnorm_dims(x):
+    if x.dim() < 2:
+        raise ValueError("group norm needs [N, ..., C]")
+    hw = 1
+    for n in x.shape[1:-1]:
+        hw *= n
+    return x.shape[0], hw, x.shape[-1]
+
+
+def ekya_op_groupnorm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5,
+                      act: int = EKYA_ACT_NONE, y=None):
+    """(y, mean, rstd) of x [N, ..., C], channels last; y may be x."""
+    torch = _torch()
+    lib = load()
+    N, HW, C = _groupnorm_dims(x)
+    _on_current(x, gamma, beta, y)
+    _shaped(gamma, (C,), "gamma"), _shaped(beta, (C,), "beta"), _shaped(y, x.shape, "y")
+    prec, f32 = _precision(x), torch.float32
+    y = torch.empty_like(x) if y is None else y
+    stats = torch.empty(2, N, max(groups, 0), dtype=f32, device=x.device)
+    mean, rstd = stats[0], stats[1]
+    nbytes = lib.ekya_op_groupnorm_workspace(prec, N, HW, C, groups)
+    ws = _scratch(nbytes, x.device)
+    _op(lib.ekya_op_groupnorm(prec, _dev(x), N, HW, C, groups, _dev(gamma, f32), _dev(beta, f32), eps,
+                              act, _dev(y, x.dtype), _dev(mean), _dev(rstd), _dev(ws), nbytes,
+                              _stream()))
+    return y, mean, rstd
+
+
+def ekya_op_groupnorm_backward(dy, x, groups: int, gamma, beta, mean, rstd,
+                               act: int = EKYA_ACT_NONE, dx=None):
+    """(dx, dgamma, dbeta); dx may be dy or x."""
+    torch = _torch()
+    lib = load()
+    N, HW, C = _groupnorm_dims(x)
+    _on_current(x, dy, gamma, beta, mean, rstd, dx)
+    _shaped(dy, x.shape, "dy"), _shaped(gamma, (C,), "gamma"), _shaped(beta, (C,), "beta")
+    _shaped(mean, (N, groups), "mean"), _shaped(rstd, (N, groups), "rstd")
+    _shaped(dx, x.shape, "dx")
+    prec, f32 = _precision(x), torch.float32
+    dx = torch.empty_like(x) if dx is None else dx
+    grads = torch.empty(2, C, dtype=f32, device=x.device)
+    dgamma, dbeta = grads[0], grads[1]
+    nbytes = lib.ekya_op_groupnorm_backward_workspace(prec, N, HW, C, groups)
+    ws = _scratch(nbytes, x.device)
+    _op(lib.ekya_op_groupnorm_backward(prec, _dev(dy, x.dtype), _dev(x), N, HW, C, groups,
+                                       _dev(gamma, f32), _dev(beta, f32), _dev(mean, f32),
+                                       _dev(rstd, f32), act, _dev(dx, x.dtype), _dev(dgamma),
+                                       _dev(dbeta), _dev(ws), nbytes, _stream()))
+    return dx, dgamma, dbeta
 
 
 # ---------------------------------------------------- scheduling layer (host)

@@ -682,6 +682,89 @@ ekya_status ekya_op_resize(int precision, const void* frames, int n, int H, int 
 
 }  // extern "C"
 
+// ------------------------------------------------ adapter-training operators
+namespace {
+
+bool aligned(const void* p, size_t n) { return reinterpret_cast<uintptr_t>(p) % n == 0; }
+
+// Whether the byte ranges [a, a + na) and [b, b + nb) share a byte.
+bool overlap(const void* a, size_t na, const void* b, size_t nb) {
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
+  return a && b && x < y + nb && y < x + na;
+}
+bool partial_overlap(const void* a, const void* b, size_t n) { return a != b && overlap(a, n, b, n); }
+
+ekya_status check_workspace(const char* op, const void* ws, size_t bytes, size_t need) {
+  if (bytes < need || (need && (!ws || !aligned(ws, 16))))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG,
+                std::string(op) + ": the workspace must hold " + std::to_string(need) +
+                    " bytes on a multiple of 16");
+  return EKYA_OK;
+}
+
+bool valid_act(int a) { return a >= EKYA_ACT_NONE && a <= EKYA_ACT_GELU; }
+
+bool groupnorm_sizes_ok(int precision, int N, long long HW, int C, int groups) {
+  return valid_precision(precision) && N >= 0 && HW >= 1 && C >= 1 && C <= 65536 && groups >= 1 &&
+         C % groups == 0 && HW <= (1LL << 40) / C && (N == 0 || HW * C <= (1LL << 40) / N);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ekya_op_groupnorm_workspace(int precision, int N, long long HW, int C, int groups) {
+  if (!groupnorm_sizes_ok(precision, N, HW, C, groups)) return 0;
+  return ekya::groupnorm_workspace_floats(precision, N, HW, C, groups, false) * sizeof(float);
+}
+
+ekya_status ekya_op_groupnorm(int precision, const void* x, int N, long long HW, int C, int groups,
+                              const float* gamma, const float* beta, float eps, int act, void* y,
+                              float* mean, float* rstd, void* workspace, size_t workspace_bytes,
+                              void* stream) {
+  if (!groupnorm_sizes_ok(precision, N, HW, C, groups) || !valid_act(act) || !(eps > 0.f) ||
+      !std::isfinite(eps) || !gamma != !beta)
+    return fail(nullptr, EKYA_ERR_INVALID_ARG, "invalid groupnorm arguments");
+  if (N == 0) return EKYA_OK;
+  const size_t e = ekya::dtype_size(precision), bytes = (size_t)N * HW * C * e;
+  if (!x || !y || !mean || !rstd || !aligned(x, e) || !aligned(y, e) || !aligned(mean, 4) ||
+      !aligned(rstd, 4) || !aligned(gamma, 4) || !aligned(beta, 4) || partial_overlap(x, y, bytes))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG, "groupnorm: null, misaligned or overlapping tensors");
+  const size_t need = ekya::groupnorm_workspace_floats(precision, N, HW, C, groups, false) * sizeof(float);
+  if (ekya_status s = check_workspace("groupnorm", workspace, workspace_bytes, need)) return s;
+  return hip_status(ekya::groupnorm_fwd(precision, x, N, HW, C, groups, gamma, beta, eps, act, y,
+                                        mean, rstd, (float*)workspace, (hipStream_t)stream));
+}
+
+size_t ekya_op_groupnorm_backward_workspace(int precision, int N, long long HW, int C, int groups) {
+  if (!groupnorm_sizes_ok(precision, N, HW, C, groups)) return 0;
+  return ekya::groupnorm_workspace_floats(precision, N, HW, C, groups, true) * sizeof(float);
+}
+
+ekya_status ekya_op_groupnorm_backward(int precision, const void* dy, const void* x, int N,
+                                       long long HW, int C, int groups, const float* gamma,
+                                       const float* beta, const float* mean, const float* rstd,
+                                       int act, void* dx, float* dgamma, float* dbeta,
+                                       void* workspace, size_t workspace_bytes, void* stream) {
+  if (!groupnorm_sizes_ok(precision, N, HW, C, groups) || !valid_act(act) || !gamma != !beta ||
+      !dgamma != !dbeta)
+    return fail(nullptr, EKYA_ERR_INVALID_ARG, "invalid groupnorm_backward arguments");
+  const size_t e = ekya::dtype_size(precision), bytes = (size_t)N * HW * C * e;
+  if ((N > 0 && (!dy || !x || !mean || !rstd || !dx)) || !aligned(dy, e) || !aligned(x, e) ||
+      !aligned(dx, e) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) ||
+      !aligned(rstd, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4) ||
+      partial_overlap(dx, dy, bytes) || partial_overlap(dx, x, bytes))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG,
+                "groupnorm_backward: null, misaligned or overlapping tensors");
+  const size_t need = ekya::groupnorm_workspace_floats(precision, N, HW, C, groups, true) * sizeof(float);
+  if (ekya_status s = check_workspace("groupnorm_backward", workspace, workspace_bytes, need)) return s;
+  return hip_status(ekya::groupnorm_bwd(precision, dy, x, N, HW, C, groups, gamma, beta, mean, rstd,
+                                        act, dx, dgamma, dbeta, (float*)workspace,
+                                        (hipStream_t)stream));
+}
+
+}  // extern "C"
+
 // ------------------------------------------------------ scheduling layer
 extern "C" {
 

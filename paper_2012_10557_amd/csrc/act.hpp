@@ -1,0 +1,59 @@
+// Activations of the epilogues and of group norm, and their derivatives, in
+// fp32 for values stored as T.
+#pragma once
+
+#include <type_traits>
+
+#include "common.hpp"
+
+namespace ekya {
+
+enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2, ACT_GELU = 3 };
+
+// 1 / (1 + exp(-u)); exp(-u) may overflow, the quotient is then 0.  bf16: the
+// hardware's exp2 and reciprocal, off by about (|u| + 2) 2^-24, far below the
+// 2^-9 of the result's rounding.
+template <typename T> __device__ __forceinline__ float sigmoid_of(float u) {
+  if constexpr (sizeof(T) == 4) return 1.f / (1.f + expf(-u));
+  return __builtin_amdgcn_rcpf(1.f + __expf(-u));
+}
+
+// (1 + erf(u / sqrt 2)) / 2.  fp32: by erfc, which keeps its digits where the
+// sum cancels (u far below 0); bf16: the sum, off by 2^-25 there.
+template <typename T> __device__ __forceinline__ float normal_cdf(float u) {
+  if constexpr (sizeof(T) == 4) return 0.5f * erfcf(-0.70710678f * u);
+  return 0.5f + 0.5f * erff(0.70710678f * u);
+}
+
+template <int ACT, typename T> __device__ __forceinline__ float act_fwd(float u) {
+  if constexpr (ACT == ACT_RELU) return relu_nan(u);
+  if constexpr (ACT == ACT_SILU) return u * sigmoid_of<T>(u);
+  if constexpr (ACT == ACT_GELU) return u * normal_cdf<T>(u);
+  return u;
+}
+
+// dy * act'(u).  A masked-out ReLU gradient is 0 even where dy is not finite.
+template <int ACT, typename T> __device__ __forceinline__ float act_bwd(float dy, float u) {
+  if constexpr (ACT == ACT_RELU) return u > 0.f ? dy : 0.f;
+  if constexpr (ACT == ACT_SILU) {
+    const float p = sigmoid_of<T>(u);
+    return dy * (p * (1.f + u * (1.f - p)));
+  }
+  if constexpr (ACT == ACT_GELU) {
+    const float e = sizeof(T) == 4 ? expf(-0.5f * u * u) : __expf(-0.5f * u * u);
+    return dy * (normal_cdf<T>(u) + u * (0.39894228f * e));
+  }
+  return dy;
+}
+
+// Calls f(std::integral_constant<int, ACT>) for a checked activation.
+template <typename F> auto act_dispatch(int act, F&& f) {
+  switch (act) {
+    case ACT_RELU: return f(std::integral_constant<int, ACT_RELU>{});
+    case ACT_SILU: return f(std::integral_constant<int, ACT_SILU>{});
+    case ACT_GELU: return f(std::integral_constant<int, ACT_GELU>{});
+    default: return f(std::integral_constant<int, ACT_NONE>{});
+  }
+}
+
+}  // namespace ekya

@@ -1,0 +1,545 @@
+// Group norm with an activation over channels-last activations, forward and
+// backward.
+//
+// Statistics pass, coefficients, apply pass.  A block takes a range of pixels
+// of one sample and up to 64 16-byte units of its channels; a thread keeps one
+// unit's channels and walks the pixels.  Sums are kept per channel, whatever
+// the group size (groups of 3 or 10 channels straddle the units), and folded
+// into groups by the coefficient kernels.  Means and squared deviations are
+// merged pairwise (Chan, Golub and LeVeque), so that a mean far from zero costs
+// no digits.
+#include <climits>
+
+#include "act.hpp"
+#include "kernels.hpp"
+
+namespace ekya {
+namespace {
+
+constexpr int GN_NT = 256;  // threads of a block
+constexpr int GN_R = 8;     // pixels a thread has in flight
+
+// E consecutive elements of a channel run: a 16-byte unit, or one element
+// where channels or addresses allow no units.
+template <typename T, int E> struct GnUnit {
+  uint4 u;
+  __device__ __forceinline__ void load(const T* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void get(float (&v)[E]) const {
+    Unit<T> t;
+    t.u = u;
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = to_f(t.e[e]);
+  }
+  static __device__ __forceinline__ void store(T* p, const float (&v)[E]) {
+    Unit<T> t;
+#pragma unroll
+    for (int e = 0; e < E; ++e) t.e[e] = from_f<T>(v[e]);
+    *reinterpret_cast<uint4*>(p) = t.u;
+  }
+};
+template <typename T> struct GnUnit<T, 1> {
+  T u;
+  __device__ __forceinline__ void load(const T* p) { u = *p; }
+  __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = to_f(u); }
+  static __device__ __forceinline__ void store(T* p, const float (&v)[1]) { *p = from_f<T>(v[0]); }
+};
+
+struct GnArgs {
+  const void *x, *dy;
+  void* out;
+  const float *gamma, *beta;  // null: 1 and 0
+  float *mean, *rstd;         // [N][G]
+  float* part;                // [N][chunks][C][2]
+  float* tot;                 // [N][C][2] (backward)
+  float* coef;                // [N][G][2] (backward)
+  float *dgamma, *dbeta;
+  long long HW;
+  int N, C, G, gs;       // gs: channels of a group
+  int cu, cup, cchunks;  // units of a channel chunk, the next power of two, chunks
+  int rows, chunks;      // pixels of a chunk, chunks of a sample
+  float eps;
+};
+
+// A block's sample, pixel range and channel unit.
+struct GnPlace {
+  int n, chunk, c;     // c: the thread's first channel
+  long long r0, r1;    // pixels
+  int r, rpp;          // the thread's row within a pass, rows of a pass
+  bool on;
+};
+template <int E> __device__ __forceinline__ GnPlace gn_place(const GnArgs& a) {
+  GnPlace p;
+  const int b = blockIdx.x, per = a.chunks * a.cchunks;
+  p.n = b / per;
+  const int rest = b - p.n * per;
+  p.chunk = rest / a.cchunks;
+  const int u = threadIdx.x & (a.cup - 1);
+  p.r = threadIdx.x / a.cup;
+  p.rpp = GN_NT / a.cup;
+  p.c = ((rest - p.chunk * a.cchunks) * a.cu + u) * E;
+  p.on = u < a.cu && p.c < a.C;
+  p.r0 = (long long)p.chunk * a.rows;
+  p.r1 = min(a.HW, p.r0 + a.rows);
+  return p;
+}
+
+// (n, mean, m2) += (nb, meanb, m2b): counts as floats, nb > 0.
+__device__ __forceinline__ void chan_merge(float& n, float& mean, float& m2, float nb, float meanb,
+                                           float m2b) {
+  const float t = n + nb, d = meanb - mean, f = t > 0.f ? nb / t : 0.f;
+  mean += d * f;
+  m2 += m2b + d * d * (n * f);
+  n = t;
+}
+
+// Sums v over the threads of a block that share a channel unit, in a fixed
+// order; threads of the first row return the totals.  red: GN_NT * E floats.
+template <int E> __device__ __forceinline__ void gn_row_sum(float (&v)[E], float* red, int cup) {
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e) red[threadIdx.x * E + e] = v[e];
+  __syncthreads();
+  for (int h = GN_NT / 2; h >= cup; h >>= 1) {
+    if ((int)threadIdx.x < h)
+#pragma unroll
+      for (int e = 0; e < E; ++e) red[threadIdx.x * E + e] += red[(threadIdx.x + h) * E + e];
+    __syncthreads();
+  }
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = red[threadIdx.x * E + e];
+}
+
+// part[n][chunk][c] = (mean, squared deviations) of the chunk's pixels.
+template <typename T, int E> __global__ __launch_bounds__(GN_NT) void gn_stats_kernel(GnArgs a) {
+  __shared__ float red[GN_NT * E];
+  const GnPlace p = gn_place<E>(a);
+  const T* x = (const T*)a.x + p.n * a.HW * a.C + p.c;
+  float cnt = 0.f, mean[E], m2[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) mean[e] = m2[e] = 0.f;
+  for (long long r = p.r0 + p.r; p.on && r < p.r1; r += (long long)GN_R * p.rpp) {
+    GnUnit<T, E> u[GN_R];
+    int k = 0;
+#pragma unroll
+    for (int i = 0; i < GN_R; ++i)
+      if (r + (long long)i * p.rpp < p.r1) {
+        u[i].load(x + (r + (long long)i * p.rpp) * a.C);
+        ++k;
+      }
+    float s[E], q[E], v[E];
+#pragma unroll
+    for (int e = 0; e < E; ++e) s[e] = q[e] = 0.f;
+#pragma unroll
+    for (int i = 0; i < GN_R; ++i)
+      if (i < k) {
+        u[i].get(v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) s[e] += v[e];
+      }
+    const float inv = 1.f / k;
+#pragma unroll
+    for (int e = 0; e < E; ++e) s[e] *= inv;
+#pragma unroll
+    for (int i = 0; i < GN_R; ++i)
+      if (i < k) {
+        u[i].get(v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) q[e] += (v[e] - s[e]) * (v[e] - s[e]);
+      }
+    const float n0 = cnt;
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      cnt = n0;
+      chan_merge(cnt, mean[e], m2[e], (float)k, s[e], q[e]);
+    }
+  }
+  // the chunk's mean, then the deviations from it
+  const float total = (float)(p.r1 - p.r0);
+  float s[E], d[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) s[e] = mean[e] * (cnt / total);
+  gn_row_sum<E>(s, red, a.cup);
+  if (p.r == 0)
+#pragma unroll
+    for (int e = 0; e < E; ++e) red[threadIdx.x * E + e] = s[e];
+  __syncthreads();
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    s[e] = red[(threadIdx.x & (a.cup - 1)) * E + e];
+    d[e] = m2[e] + cnt * (mean[e] - s[e]) * (mean[e] - s[e]);
+  }
+  gn_row_sum<E>(d, red, a.cup);
+  if (p.r == 0 && p.on) {
+    float* o = a.part + 2 * (((long long)p.n * a.chunks + p.chunk) * a.C + p.c);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      o[2 * e] = s[e];
+      o[2 * e + 1] = d[e];
+    }
+  }
+}
+
+__device__ __forceinline__ float block_sum(float v, float* red) {  // red: 4 floats
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+  __syncthreads();
+  return (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// mean and rstd of a (sample, group) from its chunks' channels: a block each.
+__global__ __launch_bounds__(GN_NT) void gn_mean_kernel(GnArgs a) {
+  __shared__ float red[4];
+  const int n = blockIdx.x / a.G, g = blockIdx.x - n * a.G;
+  const float* part = a.part + 2 * ((long long)n * a.chunks * a.C + g * a.gs);
+  const int count = a.chunks * a.gs;
+  const float inv = 1.f / ((float)a.HW * a.gs);
+  const float last = (float)(a.HW - (long long)(a.chunks - 1) * a.rows);
+  float s = 0.f;
+  for (int i = threadIdx.x; i < count; i += GN_NT) {
+    const int k = i / a.gs, c = i - k * a.gs;
+    s += part[2 * ((long long)k * a.C + c)] * ((k == a.chunks - 1 ? last : (float)a.rows) * inv);
+  }
+  const float mean = block_sum(s, red);
+  float q = 0.f;
+  for (int i = threadIdx.x; i < count; i += GN_NT) {
+    const int k = i / a.gs, c = i - k * a.gs;
+    const float* p = part + 2 * ((long long)k * a.C + c);
+    q += p[1] + (k == a.chunks - 1 ? last : (float)a.rows) * (p[0] - mean) * (p[0] - mean);
+  }
+  const float var = block_sum(q, red) * inv;
+  if (threadIdx.x == 0) {
+    a.mean[blockIdx.x] = mean;
+    a.rstd[blockIdx.x] = 1.f / sqrtf(var + a.eps);
+  }
+}
+
+// A thread's per-channel constants.
+template <int E> struct GnChan {
+  float mean[E], rstd[E], gamma[E], beta[E];
+  __device__ __forceinline__ void load(const GnArgs& a, int n, int c) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const int g = (c + e) / a.gs;
+      mean[e] = a.mean[(long long)n * a.G + g];
+      rstd[e] = a.rstd[(long long)n * a.G + g];
+      gamma[e] = a.gamma ? a.gamma[c + e] : 1.f;
+      beta[e] = a.beta ? a.beta[c + e] : 0.f;
+    }
+  }
+  __device__ __forceinline__ float xhat(int e, float x) const { return (x - mean[e]) * rstd[e]; }
+  // Rounded after every operation, so that forward and backward (and whoever
+  // follows the formula in fp32) see the same sign at a ReLU.
+  __device__ __forceinline__ float pre(int e, float xh) const {
+    return __fadd_rn(__fmul_rn(xh, gamma[e]), beta[e]);
+  }
+};
+
+template <typename T, int E, int ACT>
+__global__ __launch_bounds__(GN_NT) void gn_apply_kernel(GnArgs a) {
+  const GnPlace p = gn_place<E>(a);
+  if (!p.on) return;
+  GnChan<E> ch;
+  ch.load(a, p.n, p.c);
+  const long long base = p.n * a.HW * a.C + p.c;
+  const T* x = (const T*)a.x + base;
+  T* y = (T*)a.out + base;
+  for (long long r = p.r0 + p.r; r < p.r1; r += p.rpp) {
+    GnUnit<T, E> u;
+    float v[E];
+    u.load(x + r * a.C);
+    u.get(v);
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] = act_fwd<ACT, T>(ch.pre(e, ch.xhat(e, v[e])));
+    GnUnit<T, E>::store(y + r * a.C, v);
+  }
+}
+
+// part[n][chunk][c] = (sum g, sum g * xhat) of the chunk's pixels.
+template <typename T, int E, int ACT>
+__global__ __launch_bounds__(GN_NT) void gn_bwd_sums_kernel(GnArgs a) {
+  __shared__ float red[GN_NT * E];
+  const GnPlace p = gn_place<E>(a);
+  float s[E], q[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) s[e] = q[e] = 0.f;
+  if (p.on) {
+    GnChan<E> ch;
+    ch.load(a, p.n, p.c);
+    const long long base = p.n * a.HW * a.C + p.c;
+    const T *x = (const T*)a.x + base, *dy = (const T*)a.dy + base;
+    for (long long r = p.r0 + p.r; r < p.r1; r += p.rpp) {
+      GnUnit<T, E> ux, ud;
+      float v[E], d[E];
+      ux.load(x + r * a.C);
+      ud.load(dy + r * a.C);
+      ux.get(v);
+      ud.get(d);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float xh = ch.xhat(e, v[e]), g = act_bwd<ACT, T>(d[e], ch.pre(e, xh));
+        s[e] += g;
+        q[e] += g * xh;
+      }
+    }
+  }
+  gn_row_sum<E>(s, red, a.cup);
+  gn_row_sum<E>(q, red, a.cup);
+  if (p.r == 0 && p.on) {
+    float* o = a.part + 2 * (((long long)p.n * a.chunks + p.chunk) * a.C + p.c);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      o[2 * e] = s[e];
+      o[2 * e + 1] = q[e];
+    }
+  }
+}
+
+// tot[n][c] = sum of the sample's chunks.
+__global__ __launch_bounds__(GN_NT) void gn_bwd_fold_kernel(GnArgs a) {
+  const long long i = (long long)blockIdx.x * GN_NT + threadIdx.x, n = i / (2 * a.C);
+  if (n >= a.N) return;
+  const long long c = i - n * 2 * a.C;
+  const float* p = a.part + n * a.chunks * 2 * a.C + c;
+  float s = 0.f;
+  for (int k = 0; k < a.chunks; ++k) s += p[(long long)k * 2 * a.C];
+  a.tot[i] = s;
+}
+
+// Blocks below N * G: coef = (avg h, avg h * xhat) of a (sample, group); the
+// others: dgamma and dbeta of 64 channels, summed over the samples.
+__global__ __launch_bounds__(GN_NT) void gn_bwd_coef_kernel(GnArgs a, int groups) {
+  __shared__ float red[4][128];
+  const int t = threadIdx.x;
+  if ((int)blockIdx.x < groups) {
+    const int n = blockIdx.x / a.G, g = blockIdx.x - n * a.G;
+    const float* tot = a.tot + 2 * ((long long)n * a.C + g * a.gs);
+    float s = 0.f, q = 0.f;
+    for (int c = t; c < a.gs; c += GN_NT) {
+      const float w = a.gamma ? a.gamma[g * a.gs + c] : 1.f;
+      s += w * tot[2 * c];
+      q += w * tot[2 * c + 1];
+    }
+    s = block_sum(s, red[0]);
+    q = block_sum(q, red[0]);
+    const float inv = 1.f / ((float)a.HW * a.gs);
+    if (t == 0) {
+      a.coef[2 * (long long)blockIdx.x] = s * inv;
+      a.coef[2 * (long long)blockIdx.x + 1] = q * inv;
+    }
+    return;
+  }
+  const int c0 = ((int)blockIdx.x - groups) * 64, c = c0 + (t & 63);
+  float s = 0.f, q = 0.f;
+  if (c < a.C)
+    for (int n = t >> 6; n < a.N; n += 4) {
+      const float* p = a.tot + 2 * ((long long)n * a.C + c);
+      s += p[0];
+      q += p[1];
+    }
+  red[t >> 6][t & 63] = s;
+  red[t >> 6][64 + (t & 63)] = q;
+  __syncthreads();
+  if (t < 128 && c0 + (t & 63) < a.C)
+    (t < 64 ? a.dbeta : a.dgamma)[c0 + (t & 63)] =
+        (red[0][t] + red[1][t]) + (red[2][t] + red[3][t]);
+}
+
+template <typename T, int E, int ACT>
+__global__ __launch_bounds__(GN_NT) void gn_bwd_apply_kernel(GnArgs a) {
+  const GnPlace p = gn_place<E>(a);
+  if (!p.on) return;
+  GnChan<E> ch;
+  ch.load(a, p.n, p.c);
+  float ca[E], cb[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    const float* k = a.coef + 2 * ((long long)p.n * a.G + (p.c + e) / a.gs);
+    ca[e] = k[0];
+    cb[e] = k[1];
+  }
+  const long long base = p.n * a.HW * a.C + p.c;
+  const T *x = (const T*)a.x + base, *dy = (const T*)a.dy + base;
+  T* dx = (T*)a.out + base;
+  for (long long r = p.r0 + p.r; r < p.r1; r += p.rpp) {
+    GnUnit<T, E> ux, ud;
+    float v[E], d[E];
+    ux.load(x + r * a.C);
+    ud.load(dy + r * a.C);
+    ux.get(v);
+    ud.get(d);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      const float xh = ch.xhat(e, v[e]), h = act_bwd<ACT, T>(d[e], ch.pre(e, xh)) * ch.gamma[e];
+      v[e] = ch.rstd[e] * (h - ca[e] - xh * cb[e]);
+    }
+    GnUnit<T, E>::store(dx + r * a.C, v);
+  }
+}
+
+int next_pow2(int v) {
+  int p = 1;
+  while (p < v) p *= 2;
+  return p;
+}
+
+// How a call is cut.  Chunks of pixels: 8 per thread at least, and no more
+// than 1024 a sample, nor than give about 8 blocks per CU.
+void gn_cut(GnArgs& a, int E) {
+  const int units = a.C / E;
+  a.cchunks = cdiv(units, 64);
+  a.cu = cdiv(units, a.cchunks);
+  a.cup = next_pow2(a.cu);
+  const int rpp = GN_NT / a.cup;
+  const long long blocks = (long long)a.N * a.cchunks;
+  const long long want = std::min<long long>(1024, std::max<long long>(1, 2048 / std::max(1LL, blocks)));
+  const long long least = (long long)GN_R * rpp;
+  long long rows = std::max(least, cdivl(a.HW, want));
+  rows = cdivl(rows, least) * least;
+  a.rows = (int)std::min<long long>(rows, INT_MAX);
+  a.chunks = (int)cdivl(a.HW, a.rows);
+}
+
+bool unit_ok(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+
+// Launches `kernel` over samples of a.N in groups whose grids stay below 2^23
+// blocks; `per` blocks a sample.
+template <typename F> hipError_t gn_samples(GnArgs a, size_t esize, long long per, F&& go) {
+  const long long most = std::max<long long>(1, (1 << 23) / per), N = a.N;
+  for (long long n = 0; n < N; n += most) {
+    GnArgs b = a;
+    b.N = (int)std::min(most, N - n);
+    const size_t off = (size_t)n * a.HW * a.C * esize;
+    b.x = (const char*)a.x + off;
+    if (a.dy) b.dy = (const char*)a.dy + off;
+    b.out = (char*)a.out + off;
+    b.mean = a.mean + n * a.G;
+    b.rstd = a.rstd + n * a.G;
+    b.part = a.part + n * a.chunks * 2 * a.C;
+    if (a.tot) b.tot = a.tot + n * 2 * a.C;
+    if (a.coef) b.coef = a.coef + n * 2 * a.G;
+    EKYA_HIP(go(b, dim3((unsigned)(b.N * per))));
+  }
+  return hipSuccess;
+}
+
+template <typename T, int E> hipError_t gn_forward(GnArgs a, int act, hipStream_t st) {
+  gn_cut(a, E);
+  const long long per = (long long)a.chunks * a.cchunks;
+  EKYA_HIP(gn_samples(a, sizeof(T), per, [&](const GnArgs& b, dim3 grid) {
+    hipLaunchKernelGGL((gn_stats_kernel<T, E>), grid, dim3(GN_NT), 0, st, b);
+    return hipGetLastError();
+  }));
+  EKYA_HIP(gn_samples(a, sizeof(T), a.G, [&](const GnArgs& b, dim3 grid) {
+    hipLaunchKernelGGL(gn_mean_kernel, grid, dim3(GN_NT), 0, st, b);
+    return hipGetLastError();
+  }));
+  return gn_samples(a, sizeof(T), per, [&](const GnArgs& b, dim3 grid) {
+    return act_dispatch(act, [&](auto k) {
+      hipLaunchKernelGGL((gn_apply_kernel<T, E, k.value>), grid, dim3(GN_NT), 0, st, b);
+      return hipGetLastError();
+    });
+  });
+}
+
+template <typename T, int E> hipError_t gn_backward(GnArgs a, int act, hipStream_t st) {
+  gn_cut(a, E);
+  const long long per = (long long)a.chunks * a.cchunks;
+  EKYA_HIP(gn_samples(a, sizeof(T), per, [&](const GnArgs& b, dim3 grid) {
+    return act_dispatch(act, [&](auto k) {
+      hipLaunchKernelGGL((gn_bwd_sums_kernel<T, E, k.value>), grid, dim3(GN_NT), 0, st, b);
+      return hipGetLastError();
+    });
+  }));
+  EKYA_HIP(gn_samples(a, sizeof(T), cdiv(2 * a.C, GN_NT), [&](const GnArgs& b, dim3) {
+    hipLaunchKernelGGL(gn_bwd_fold_kernel, dim3((unsigned)cdivl((long long)b.N * 2 * a.C, GN_NT)),
+                       dim3(GN_NT), 0, st, b);
+    return hipGetLastError();
+  }));
+  const int dparam = a.dgamma ? cdiv(a.C, 64) : 0;
+  EKYA_HIP(gn_samples(a, sizeof(T), a.G, [&](const GnArgs& b, dim3 grid) {
+    hipLaunchKernelGGL(gn_bwd_coef_kernel, grid, dim3(GN_NT), 0, st, b, (int)grid.x);
+    return hipGetLastError();
+  }));
+  if (dparam) {
+    hipLaunchKernelGGL(gn_bwd_coef_kernel, dim3(dparam), dim3(GN_NT), 0, st, a, 0);
+    EKYA_HIP(hipGetLastError());
+  }
+  return gn_samples(a, sizeof(T), per, [&](const GnArgs& b, dim3 grid) {
+    return act_dispatch(act, [&](auto k) {
+      hipLaunchKernelGGL((gn_bwd_apply_kernel<T, E, k.value>), grid, dim3(GN_NT), 0, st, b);
+      return hipGetLastError();
+    });
+  });
+}
+
+GnArgs gn_args(int N, long long HW, int C, int G) {
+  GnArgs a{};
+  a.N = N;
+  a.HW = HW;
+  a.C = C;
+  a.G = G;
+  a.gs = C / G;
+  return a;
+}
+
+size_t gn_part_floats(GnArgs a, int E) {
+  gn_cut(a, E);
+  return (size_t)a.N * a.chunks * 2 * a.C;
+}
+
+}  // namespace
+
+// Scratch in floats, for either unit (addresses decide which one a call takes).
+size_t groupnorm_workspace_floats(int dt, int N, long long HW, int C, int G, bool backward) {
+  const GnArgs a = gn_args(N, HW, C, G);
+  const int E = dtype_vec(dt);
+  size_t f = gn_part_floats(a, 1);
+  if (C % E == 0) f = std::max(f, gn_part_floats(a, E));
+  if (backward) f += (size_t)N * 2 * (C + (size_t)G);
+  return f;
+}
+
+hipError_t groupnorm_fwd(int dt, const void* x, int N, long long HW, int C, int G,
+                         const float* gamma, const float* beta, float eps, int act, void* y,
+                         float* mean, float* rstd, float* ws, hipStream_t st) {
+  GnArgs a = gn_args(N, HW, C, G);
+  a.x = x;
+  a.out = y;
+  a.gamma = gamma;
+  a.beta = beta;
+  a.eps = eps;
+  a.mean = mean;
+  a.rstd = rstd;
+  a.part = ws;
+  const bool unit = C % dtype_vec(dt) == 0 && unit_ok(x) && unit_ok(y);
+  if (dt == DT_BF16)
+    return unit ? gn_forward<bf16, 8>(a, act, st) : gn_forward<bf16, 1>(a, act, st);
+  return unit ? gn_forward<float, 4>(a, act, st) : gn_forward<float, 1>(a, act, st);
+}
+
+hipError_t groupnorm_bwd(int dt, const void* dy, const void* x, int N, long long HW, int C, int G,
+                         const float* gamma, const float* beta, const float* mean,
+                         const float* rstd, int act, void* dx, float* dgamma, float* dbeta,
+                         float* ws, hipStream_t st) {
+  GnArgs a = gn_args(N, HW, C, G);
+  a.x = x;
+  a.dy = dy;
+  a.out = dx;
+  a.gamma = gamma;
+  a.beta = beta;
+  a.mean = const_cast<float*>(mean);
+  a.rstd = const_cast<float*>(rstd);
+  a.dgamma = dgamma;
+  a.dbeta = dbeta;
+  a.tot = ws;
+  a.coef = a.tot + (size_t)N * 2 * C;
+  a.part = a.coef + (size_t)N * 2 * G;
+  const bool unit = C % dtype_vec(dt) == 0 && unit_ok(x) && unit_ok(dy) && unit_ok(dx);
+  if (dt == DT_BF16)
+    return unit ? gn_backward<bf16, 8>(a, act, st) : gn_backward<bf16, 1>(a, act, st);
+  return unit ? gn_backward<float, 4>(a, act, st) : gn_backward<float, 1>(a, act, st);
+}
+
+}  // namespace ekya

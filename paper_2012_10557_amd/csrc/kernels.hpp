@@ -379,6 +379,19 @@ bool pack_crsk_ok(int taps);
 hipError_t pack_crsk(int dt, const float* canonical, const LayoutTable& tab, void* shadow,
                      hipStream_t stream);
 
+// ------------------------------------------------------ adapter training
+// Group norm with an activation (act.hpp) over x [N][HW][C], channels last, and
+// its gradient (elements of `dt`; gamma and beta fp32 or null).  `ws` holds
+// groupnorm_workspace_floats floats on 16 bytes.
+size_t groupnorm_workspace_floats(int dt, int N, long long HW, int C, int G, bool backward);
+hipError_t groupnorm_fwd(int dt, const void* x, int N, long long HW, int C, int G,
+                         const float* gamma, const float* beta, float eps, int act, void* y,
+                         float* mean, float* rstd, float* ws, hipStream_t stream);
+hipError_t groupnorm_bwd(int dt, const void* dy, const void* x, int N, long long HW, int C, int G,
+                         const float* gamma, const float* beta, const float* mean,
+                         const float* rstd, int act, void* dx, float* dgamma, float* dbeta,
+                         float* ws, hipStream_t stream);
+
 // ------------------------------------------------------------- diagnostics
 // n one-wavefront workgroups; workgroup i writes the compute unit it ran on,
 // (xcd << 10) | (shader array << 8) | (shader engine << 4) | cu, to out[i].
