@@ -102,7 +102,7 @@ ekya_status ekya_op_resize(int precision, const void* frames, int n, int H, int 
 /* ------------------------------------------------- adapter-training operators
  * What fine-tuning an adapter or a head on the network's features needs beside
  * the layers above: group norm in place of BatchNorm (whose batch statistics
- * say little on a few frames).
+ * say little on a few frames), and AdamW.
  *
  * These calls are asynchronous: they queue kernels on `stream` (of the current
  * device), allocate nothing, copy nothing and never wait, so they can be
@@ -145,6 +145,59 @@ ekya_status ekya_op_groupnorm_backward(int precision, const void* dy, const void
                                        const float* beta, const float* mean, const float* rstd,
                                        int act, void* dx, float* dgamma, float* dbeta,
                                        void* workspace, size_t workspace_bytes, void* stream);
+
+/* AdamW over a list of tensors.  For every element, with t = step:
+ *   m = beta1 m + (1 - beta1) g          v = beta2 v + (1 - beta2) g^2
+ *   w = w (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
+ * w is fp32; g is fp32 or bf16; `low`, where given, receives w rounded to bf16
+ * (the copy that products in bf16 read).
+ * state_bits 32: m and v are fp32 [n].
+ * state_bits 8: m holds n e4m3 and v n e5m2 bytes (OCP formats); element i
+ * stands for its byte's value times scale[2 (i / 256)] (m) or
+ * scale[2 (i / 256) + 1] (v), fp32 powers of two that a step rewrites: the
+ * largest finite value of the block then lies in [128, 256) or [2^14, 2^15) of
+ * its scale (a scale is at least 2^-126).  The step rounds the new states
+ * stochastically, since rounding to nearest would leave v where it is (beta2
+ * = 0.999 moves it by a thousandth, half a unit of e5m2 is an eighth): a
+ * magnitude goes up with the probability of its remainder.  The 16 random bits
+ * of element i of the list are bits 16 (i mod 4) .. of output i / 4 of the
+ * SplitMix64 stream that starts at seed + step * 0xD1B54A32D192ED03, elements
+ * counted from one tensor to the next with every tensor filled up to a
+ * multiple of 256; v takes their complement.  A v above zero is never rounded
+ * to zero (w would move by lr / eps).  Non-finite states are stored as NaN and
+ * stay out of their block's scale.  New states are zero bytes with any finite
+ * scale. */
+typedef struct {
+  float* w;
+  const void* g;
+  void* m;
+  void* v;
+  float* scale;   /* [2 * ceil(n / 256)] (state_bits 8), else null */
+  void* low;      /* bf16 [n], or null */
+  long long n;    /* 0 .. 2^38 elements */
+  float weight_decay; /* >= 0 */
+} ekya_adamw_tensor;
+typedef struct {
+  double lr, beta1, beta2, eps; /* lr >= 0, betas in [0, 1), eps >= 0 */
+  long long step;               /* 1, 2, ...; used where step_device is null */
+  const int64_t* step_device;   /* device, or null: the step's number is read on the GPU when
+                                   the kernels run, so that a replayed graph can count on;
+                                   below 1 it counts as 1 */
+  uint64_t seed;                /* stochastic rounding (state_bits 8) */
+} ekya_adamw_opts;
+typedef struct ekya_adamw ekya_adamw;
+/* The list is checked and kept (host memory only); the tensors stay the
+ * caller's.  count 0 .. 65536.  EKYA_ERR_INVALID_ARG where a tensor that a step
+ * writes overlaps another of the list.  Steps of one handle may be queued from
+ * several threads; set_grads needs the handle to itself. */
+ekya_status ekya_adamw_create(ekya_adamw** out, const ekya_adamw_tensor* tensors, int count,
+                              int grad_precision, int state_bits);
+void ekya_adamw_destroy(ekya_adamw* opt);
+/* New gradient tensors (count and sizes as created).  A step takes those that
+ * are set when it is called. */
+ekya_status ekya_adamw_set_grads(ekya_adamw* opt, const void* const* grads, int count);
+/* One step over every tensor, asynchronous on `stream`, no workspace. */
+ekya_status ekya_adamw_step(const ekya_adamw* opt, const ekya_adamw_opts* opts, void* stream);
 
 #ifdef __cplusplus
 }

@@ -95,6 +95,18 @@ class ScheduleOut(ctypes.Structure):
                 ("video_accuracy", ctypes.POINTER(ctypes.c_double)), ("accuracy", ctypes.c_double)]
 
 
+class AdamwTensor(ctypes.Structure):
+    _fields_ = [("w", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("low", ctypes.c_void_p),
+                ("n", ctypes.c_longlong), ("weight_decay", ctypes.c_float)]
+
+
+class AdamwOpts(ctypes.Structure):
+    _fields_ = [("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double), ("step", ctypes.c_longlong),
+                ("step_device", ctypes.c_void_p), ("seed", ctypes.c_uint64)]
+
+
 _P = ctypes.c_void_p
 _I = ctypes.c_int
 _LL = ctypes.c_longlong
@@ -174,6 +186,10 @@ _SIGS = {
     "ekya_op_groupnorm_backward_workspace": (ctypes.c_size_t, [_I, _I, _LL, _I, _I]),
     "ekya_op_groupnorm_backward": (_I, [_I, _P, _P, _I, _LL, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P,
                                         _P, ctypes.c_size_t, _P]),
+    "ekya_adamw_create": (_I, [ctypes.POINTER(_P), ctypes.POINTER(AdamwTensor), _I, _I, _I]),
+    "ekya_adamw_destroy": (None, [_P]),
+    "ekya_adamw_set_grads": (_I, [_P, ctypes.POINTER(_P), _I]),
+    "ekya_adamw_step": (_I, [_P, ctypes.POINTER(AdamwOpts), _P]),
 }
 
 _lib: Optional[ctypes.CDLL] = None
@@ -766,6 +782,87 @@ def ekya_op_groupnorm_backward(dy, x, groups: int, gamma, beta, mean, rstd,
                                        _dev(rstd, f32), act, _dev(dx, x.dtype), _dev(dgamma),
                                        _dev(dbeta), _dev(ws), nbytes, _stream()))
     return dx, dgamma, dbeta
+
+
+class Adamw:
+    """An optimizer handle (ekya_adamw_create): keeps its tensors alive and is
+    freed with the last reference."""
+
+    def __init__(self, handle, tensors, grads):
+        self.handle, self.tensors, self.grads = handle, tensors, grads
+        self.device = grads[0].device if grads else None
+
+    def close(self) -> None:
+        handle, self.handle = self.handle, None
+        if handle:
+            load().ekya_adamw_destroy(handle)
+
+    __del__ = close
+
+
+def _adamw_grad(g, like, dtype):
+    if tuple(g.shape) != tuple(like.shape):
+        raise ValueError(f"gradient: expected shape {tuple(like.shape)}, got {tuple(g.shape)}")
+    _on_current(like, g)
+    return _dev(g, dtype)
+
+
+def ekya_adamw_create(tensors: Sequence[dict], state_bits: int = 32) -> Adamw:
+    """tensors: dicts of w (fp32), g (fp32 or bf16), m and v (fp32; with 8 bits
+    float8_e4m3fn and float8_e5m2), and as needed scale (8 bits: fp32
+    [ceil(n / 256), 2]), low (bf16) and weight_decay."""
+    torch = _torch()
+    if state_bits not in (8, 32):
+        raise ValueError("state_bits must be 8 or 32")
+    kinds = (torch.float8_e4m3fn, torch.float8_e5m2) if state_bits == 8 else (torch.float32,) * 2
+    arr = (AdamwTensor * max(1, len(tensors)))()
+    gtype = tensors[0]["g"].dtype if tensors else torch.float32
+    for a, t in zip(arr, tensors):
+        w, m, v, scale, low = t["w"], t["m"], t["v"], t.get("scale"), t.get("low")
+        _on_current(w, m, v, scale, low)
+        _shaped(m, w.shape, "m"), _shaped(v, w.shape, "v"), _shaped(low, w.shape, "low")
+        if scale is not None and scale.numel() != (w.numel() + 255) // 256 * 2:
+            raise ValueError("scale: expected two per 256 elements")
+        a.w, a.m, a.v = _dev(w, torch.float32), _dev(m, kinds[0]), _dev(v, kinds[1])
+        a.g = _adamw_grad(t["g"], w, gtype)
+        a.scale, a.low = _dev(scale, torch.float32), _dev(low, torch.bfloat16)
+        a.n, a.weight_decay = w.numel(), t.get("weight_decay", 0.0)
+    h = ctypes.c_void_p()
+    prec = EKYA_FP32 if gtype == torch.float32 else EKYA_BF16 if gtype == torch.bfloat16 else -1
+    _op(load().ekya_adamw_create(ctypes.byref(h), arr, len(tensors), prec, state_bits))
+    return Adamw(h, list(tensors), [t["g"] for t in tensors])
+
+
+def ekya_adamw_destroy(opt: Adamw) -> None:
+    opt.close()
+
+
+def ekya_adamw_set_grads(opt: Adamw, grads: Sequence) -> None:
+    """New gradient tensors of the same shapes and type; later steps take them."""
+    if len(grads) != len(opt.tensors):
+        raise ValueError("one gradient per tensor")
+    arr = (_P * max(1, len(grads)))()
+    for i, (g, t) in enumerate(zip(grads, opt.tensors)):
+        arr[i] = _adamw_grad(g, t["w"], opt.grads[0].dtype)
+    _op(load().ekya_adamw_set_grads(opt.handle, arr, len(grads)))
+    opt.grads = list(grads)
+
+
+def ekya_adamw_step(opt: Adamw, lr: float, beta1: float = 0.9, beta2: float = 0.999,
+                    eps: float = 1e-8, step: int = 1, step_device=None, seed: int = 0) -> None:
+    """One step over every tensor.  step_device: an int64 tensor of one element on
+    the GPU that holds the step's number when the kernels run."""
+    torch = _torch()
+    if opt.device is not None and opt.device.index != torch.cuda.current_device():
+        raise ValueError("the optimizer's tensors live on another GPU")
+    if step_device is not None:
+        if step_device.numel() != 1:
+            raise ValueError("step_device: expected one element")
+        if opt.device is not None and step_device.device != opt.device:
+            raise ValueError("tensors must live on one GPU")
+        step_device = _dev(step_device, torch.int64)
+    opts = AdamwOpts(lr, beta1, beta2, eps, step, step_device, seed)
+    _op(load().ekya_adamw_step(opt.handle, ctypes.byref(opts), _stream()))
 
 
 # ---------------------------------------------------- scheduling layer (host)

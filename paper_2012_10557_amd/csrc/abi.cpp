@@ -9,6 +9,7 @@
 #include <mutex>
 #include <new>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "../../include/ekya.h"
@@ -25,6 +26,12 @@ struct ekya_ctx {
 
 struct ekya_model {
   ekya::Model m;
+};
+
+struct ekya_adamw {
+  std::vector<ekya::AdamwTensor> t;
+  std::vector<std::pair<uintptr_t, uintptr_t>> written;  // [from, to), ascending, disjoint
+  int grad_precision, state_bits;
 };
 
 namespace {
@@ -761,6 +768,112 @@ ekya_status ekya_op_groupnorm_backward(int precision, const void* dy, const void
   return hip_status(ekya::groupnorm_bwd(precision, dy, x, N, HW, C, groups, gamma, beta, mean, rstd,
                                         act, dx, dgamma, dbeta, (float*)workspace,
                                         (hipStream_t)stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+using Range = std::pair<uintptr_t, uintptr_t>;
+
+// Whether [p, p + bytes) meets one of the ascending, disjoint ranges.
+bool meets(const std::vector<Range>& ranges, const void* p, size_t bytes) {
+  const uintptr_t from = reinterpret_cast<uintptr_t>(p);
+  auto it = std::upper_bound(ranges.begin(), ranges.end(), Range(from, UINTPTR_MAX));
+  if (it != ranges.end() && it->first < from + bytes) return true;
+  return it != ranges.begin() && std::prev(it)->second > from;
+}
+
+ekya_status adamw_fill(ekya_adamw& o, const ekya_adamw_tensor* tensors, int count) {
+  const size_t gs = ekya::dtype_size(o.grad_precision), ss = o.state_bits == 8 ? 1 : 4;
+  o.t.reserve(count);
+  for (int i = 0; i < count; ++i) {
+    const ekya_adamw_tensor& t = tensors[i];
+    const std::string name = "adamw tensor " + std::to_string(i);
+    if (t.n < 0 || t.n > (1LL << 38) || !(t.weight_decay >= 0.f) || !std::isfinite(t.weight_decay))
+      return fail(nullptr, EKYA_ERR_INVALID_ARG, name + ": invalid size or weight decay");
+    if (t.n > 0 && (!t.w || !t.g || !t.m || !t.v || (o.state_bits == 8) != (t.scale != nullptr)))
+      return fail(nullptr, EKYA_ERR_INVALID_ARG, name + ": a tensor is missing, or not for these states");
+    if (!aligned(t.w, 4) || !aligned(t.g, gs) || !aligned(t.m, ss) || !aligned(t.v, ss) ||
+        !aligned(t.scale, 4) || !aligned(t.low, 2))
+      return fail(nullptr, EKYA_ERR_INVALID_ARG, name + ": misaligned");
+    o.t.push_back({t.w, t.g, t.m, t.v, t.scale, t.low, t.n, t.weight_decay});
+    if (t.n == 0) continue;
+    const std::pair<const void*, size_t> outs[] = {
+        {t.w, t.n * 4}, {t.m, t.n * ss}, {t.v, t.n * ss}, {t.low, t.n * 2},
+        {t.scale, (t.n + 255) / 256 * 8}};
+    for (const auto& p : outs)
+      if (p.first)
+        o.written.emplace_back(reinterpret_cast<uintptr_t>(p.first),
+                               reinterpret_cast<uintptr_t>(p.first) + p.second);
+  }
+  std::sort(o.written.begin(), o.written.end());
+  for (size_t i = 1; i < o.written.size(); ++i)
+    if (o.written[i].first < o.written[i - 1].second)
+      return fail(nullptr, EKYA_ERR_INVALID_ARG, "adamw: tensors that a step writes overlap");
+  return EKYA_OK;
+}
+
+ekya_status adamw_check_grad(const ekya_adamw& o, int i, const void* g) {
+  const size_t gs = ekya::dtype_size(o.grad_precision);
+  if (o.t[i].n == 0) return EKYA_OK;
+  if (!g || !aligned(g, gs) || meets(o.written, g, o.t[i].n * gs))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG,
+                "adamw gradient " + std::to_string(i) +
+                    ": null, misaligned or overlapping a tensor that a step writes");
+  return EKYA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+ekya_status ekya_adamw_create(ekya_adamw** out, const ekya_adamw_tensor* tensors, int count,
+                              int grad_precision, int state_bits) {
+  if (!out) return fail(nullptr, EKYA_ERR_INVALID_ARG, "out is null");
+  *out = nullptr;
+  if (count < 0 || count > 65536 || (count > 0 && !tensors) || !valid_precision(grad_precision) ||
+      (state_bits != 8 && state_bits != 32))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG, "invalid adamw arguments");
+  ekya_adamw* o = nullptr;
+  try {
+    o = new ekya_adamw{{}, {}, grad_precision, state_bits};
+    ekya_status s = adamw_fill(*o, tensors, count);
+    for (int i = 0; i < count && s == EKYA_OK; ++i) s = adamw_check_grad(*o, i, tensors[i].g);
+    if (s != EKYA_OK) {
+      delete o;
+      return s;
+    }
+  } catch (const std::bad_alloc&) {
+    delete o;
+    return fail(nullptr, EKYA_ERR_NOMEM, "host allocation failed");
+  }
+  *out = o;
+  return EKYA_OK;
+}
+
+void ekya_adamw_destroy(ekya_adamw* opt) { delete opt; }
+
+ekya_status ekya_adamw_set_grads(ekya_adamw* opt, const void* const* grads, int count) {
+  if (!opt || count != (int)opt->t.size() || (count > 0 && !grads))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG, "adamw_set_grads: one gradient per tensor");
+  for (int i = 0; i < count; ++i)
+    if (ekya_status s = adamw_check_grad(*opt, i, grads[i])) return s;
+  for (int i = 0; i < count; ++i) opt->t[i].g = grads[i];
+  return EKYA_OK;
+}
+
+ekya_status ekya_adamw_step(const ekya_adamw* opt, const ekya_adamw_opts* opts, void* stream) {
+  if (!opt || !opts) return fail(nullptr, EKYA_ERR_INVALID_ARG, "adamw_step: opt or opts is null");
+  if (!(opts->lr >= 0) || !std::isfinite((float)opts->lr) || !(opts->beta1 >= 0 && opts->beta1 < 1) ||
+      !(opts->beta2 >= 0 && opts->beta2 < 1) || !(opts->eps >= 0) ||
+      !std::isfinite((float)opts->eps) || (!opts->step_device && opts->step < 1) ||
+      !aligned(opts->step_device, 8))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG, "invalid adamw_step options");
+  return hip_status(ekya::adamw_step(opt->t.data(), (int)opt->t.size(), opt->grad_precision,
+                                     opt->state_bits, opts->lr, opts->beta1, opts->beta2, opts->eps,
+                                     opts->step, opts->step_device, opts->seed,
+                                     (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -392,6 +392,22 @@ hipError_t groupnorm_bwd(int dt, const void* dy, const void* x, int N, long long
                          const float* rstd, int act, void* dx, float* dgamma, float* dbeta,
                          float* ws, hipStream_t stream);
 
+// One AdamW step over tensors whose states are fp32 (bits 32) or 8-bit codes
+// with scales (bits 8); gradients of grad_dt.  step_device: the step's number
+// is read there when the kernels run (null: `step`).
+struct AdamwTensor {
+  float* w;
+  const void* g;
+  void *m, *v;
+  float* scale;
+  void* low;  // bf16, or null
+  long long n;
+  float weight_decay;
+};
+hipError_t adamw_step(const AdamwTensor* t, int count, int grad_dt, int bits, double lr,
+                      double beta1, double beta2, double eps, long long step,
+                      const int64_t* step_device, uint64_t seed, hipStream_t stream);
+
 // ------------------------------------------------------------- diagnostics
 // n one-wavefront workgroups; workgroup i writes the compute unit it ran on,
 // (xcd << 10) | (shader array << 8) | (shader engine << 4) | cu, to out[i].

@@ -47,3 +47,53 @@ def test_no_samples_need_no_tensors():
     assert lib.ekya_op_groupnorm_workspace(1, 2, 8, 32, 5) == 0
     assert lib.ekya_op_groupnorm_backward_workspace(7, 2, 8, 32, 4) == 0
     assert lib.ekya_op_groupnorm_workspace(1, 2, 8, 32, 4) > 0
+
+
+def _adamw_tensor(**kw):
+    t = dict(w=1 << 20, g=1 << 21, m=1 << 22, v=1 << 23, scale=None, low=1 << 24, n=1000,
+             weight_decay=0.0)
+    t.update(kw)
+    return binding.AdamwTensor(**t)
+
+
+def _adamw(tensors, prec=0, bits=32, count=None):
+    h = ctypes.c_void_p()
+    arr = (binding.AdamwTensor * max(1, len(tensors)))(*tensors)
+    st = binding.load().ekya_adamw_create(ctypes.byref(h), arr, len(tensors) if count is None else count,
+                                          prec, bits)
+    assert (st == binding.EKYA_OK) == bool(h)
+    return st, h
+
+
+@pytest.mark.parametrize("bad", [
+    dict(w=None), dict(g=None), dict(m=None), dict(v=None), dict(n=-1), dict(n=(1 << 38) + 1),
+    dict(scale=1 << 25), dict(weight_decay=-0.1), dict(weight_decay=float("nan")),
+    dict(w=(1 << 20) + 2), dict(low=(1 << 24) + 1), dict(m=(1 << 20) + 3996), dict(g=(1 << 20) + 3996),
+    dict(g=(1 << 22) - 3996), dict(low=1 << 23)])
+def test_adamw_refuses(bad):
+    assert _adamw([_adamw_tensor(**bad)])[0] == binding.EKYA_ERR_INVALID_ARG
+
+
+def test_adamw_list_and_options():
+    lib = binding.load()
+    assert _adamw([_adamw_tensor()] * 2)[0] == binding.EKYA_ERR_INVALID_ARG  # the same tensor twice
+    assert _adamw([_adamw_tensor()], prec=2)[0] == binding.EKYA_ERR_INVALID_ARG
+    assert _adamw([_adamw_tensor()], bits=16)[0] == binding.EKYA_ERR_INVALID_ARG
+    assert _adamw([_adamw_tensor()], bits=8)[0] == binding.EKYA_ERR_INVALID_ARG  # no scale
+    assert _adamw([], count=-1)[0] == binding.EKYA_ERR_INVALID_ARG
+    assert _adamw([], count=65537)[0] == binding.EKYA_ERR_INVALID_ARG
+    st, h = _adamw([_adamw_tensor(scale=1 << 25), _adamw_tensor(w=0, g=0, m=0, v=0, low=0, n=0)], bits=8)
+    assert st == binding.EKYA_OK
+    P2 = ctypes.c_void_p * 2
+    assert lib.ekya_adamw_set_grads(h, P2(1 << 26, None), 2) == binding.EKYA_OK
+    for grads, count in ((P2(1 << 26, None), 1), (P2(None, None), 2), (P2(1 << 22, None), 2),
+                         (P2((1 << 25) + 8, None), 2), (P2((1 << 26) + 2, None), 2)):
+        assert lib.ekya_adamw_set_grads(h, grads, count) == binding.EKYA_ERR_INVALID_ARG
+    good = dict(lr=1e-3, beta1=0.9, beta2=0.999, eps=1e-8, step=1, step_device=None, seed=0)
+    for bad in (dict(lr=-1.0), dict(lr=float("inf")), dict(lr=1e39), dict(beta1=1.0), dict(beta2=-0.1),
+                dict(beta2=float("nan")), dict(eps=-1e-8), dict(step=0), dict(step_device=4)):
+        opts = binding.AdamwOpts(**dict(good, **bad))
+        assert lib.ekya_adamw_step(h, ctypes.byref(opts), None) == binding.EKYA_ERR_INVALID_ARG, bad
+    assert lib.ekya_adamw_step(None, ctypes.byref(binding.AdamwOpts(**good)), None) != binding.EKYA_OK
+    lib.ekya_adamw_destroy(h)
+    lib.ekya_adamw_destroy(None)
