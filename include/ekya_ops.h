@@ -102,7 +102,8 @@ ekya_status ekya_op_resize(int precision, const void* frames, int n, int H, int 
 /* ------------------------------------------------- adapter-training operators
  * What fine-tuning an adapter or a head on the network's features needs beside
  * the layers above: group norm in place of BatchNorm (whose batch statistics
- * say little on a few frames), and AdamW.
+ * say little on a few frames), matrix products in the activations' type with
+ * everything elementwise behind them in the same pass, and AdamW.
  *
  * These calls are asynchronous: they queue kernels on `stream` (of the current
  * device), allocate nothing, copy nothing and never wait, so they can be
@@ -146,11 +147,73 @@ ekya_status ekya_op_groupnorm_backward(int precision, const void* dy, const void
                                        int act, void* dx, float* dgamma, float* dbeta,
                                        void* workspace, size_t workspace_bytes, void* stream);
 
+/* Matrix product with its epilogue: s = x w^T + bias, y = act(s) + residual,
+ * or, with residual_first, s = x w^T + bias + residual, y = act(s) (the order
+ * of a residual block).  Rows of a matrix are `ld` elements apart, ld >= its
+ * width; what lies between them is neither read nor written.  Products are
+ * summed in fp32; y and z are rounded once, from that.  Outputs overlap
+ * nothing else, but for y, which may be the residual (same start, same ld);
+ * columns of one buffer are fine where the lds are equal.  M times the larger
+ * of N and K is at most 2^40. */
+typedef struct {
+  int precision;        /* of x, w, residual, y and z */
+  long long M;          /* rows, >= 0 (0: nothing is done) */
+  int N, K;             /* outputs and inputs of a row, in [1, 2^24] */
+  const void* x;        /* [M][K] */
+  long long ldx;
+  const void* w;        /* [N][K] */
+  long long ldw;
+  const float* bias;    /* [N] fp32, or null */
+  int act;              /* ekya_act */
+  const void* residual; /* [M][N], or null */
+  long long ldr;
+  int residual_first;
+  void* y;              /* [M][N] */
+  long long ldy;
+  void* z;              /* [M][N], or null: receives s, which the backward pass reads */
+  long long ldz;
+} ekya_matmul_args;
+size_t ekya_op_matmul_workspace(const ekya_matmul_args* args);
+ekya_status ekya_op_matmul(const ekya_matmul_args* args, void* workspace, size_t workspace_bytes,
+                           void* stream);
+
+/* Its gradient.  dz = dy * act'(z) is the gradient of s (and of the residual
+ * where it was added first; otherwise the residual's is dy): dx = dz w, dw =
+ * dz^T x, db = sum over rows of dy * act'(z).  dz is stored in `precision` and
+ * the products read it as stored; db is summed before that rounding.  With
+ * EKYA_ACT_NONE dz is dy: z and dz are not used.  Any of dx, dw, db may be
+ * null (x is read for dw only, w for dx only).  M = 0 makes dw and db zero.
+ * Overlaps as above: dz may be dy or z. */
+typedef struct {
+  int precision;    /* of dy, z, x, w, dz and dx */
+  long long M;
+  int N, K;
+  const void* dy;   /* [M][N] */
+  long long lddy;
+  const void* z;    /* [M][N], as stored by ekya_op_matmul */
+  long long ldz;
+  int act;
+  const void* x;    /* [M][K] */
+  long long ldx;
+  const void* w;    /* [N][K] */
+  long long ldw;
+  void* dz;         /* [M][N]; may be dy or z (with its ld) */
+  long long lddz;
+  void* dx;         /* [M][K] */
+  long long lddx;
+  void* dw;         /* [N][K], rows next to each other */
+  int dw_precision; /* EKYA_FP32, or `precision` */
+  float* db;        /* [N] fp32 */
+} ekya_matmul_backward_args;
+size_t ekya_op_matmul_backward_workspace(const ekya_matmul_backward_args* args);
+ekya_status ekya_op_matmul_backward(const ekya_matmul_backward_args* args, void* workspace,
+                                    size_t workspace_bytes, void* stream);
+
 /* AdamW over a list of tensors.  For every element, with t = step:
  *   m = beta1 m + (1 - beta1) g          v = beta2 v + (1 - beta2) g^2
  *   w = w (1 - lr weight_decay) - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
  * w is fp32; g is fp32 or bf16; `low`, where given, receives w rounded to bf16
- * (the copy that products in bf16 read).
+ * (the copy that ekya_op_matmul reads).
  * state_bits 32: m and v are fp32 [n].
  * state_bits 8: m holds n e4m3 and v n e5m2 bytes (OCP formats); element i
  * stands for its byte's value times scale[2 (i / 256)] (m) or

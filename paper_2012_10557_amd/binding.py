@@ -95,6 +95,25 @@ class ScheduleOut(ctypes.Structure):
                 ("video_accuracy", ctypes.POINTER(ctypes.c_double)), ("accuracy", ctypes.c_double)]
 
 
+class MatmulArgs(ctypes.Structure):
+    _fields_ = [("precision", ctypes.c_int), ("M", ctypes.c_longlong), ("N", ctypes.c_int),
+                ("K", ctypes.c_int), ("x", ctypes.c_void_p), ("ldx", ctypes.c_longlong),
+                ("w", ctypes.c_void_p), ("ldw", ctypes.c_longlong), ("bias", ctypes.c_void_p),
+                ("act", ctypes.c_int), ("residual", ctypes.c_void_p), ("ldr", ctypes.c_longlong),
+                ("residual_first", ctypes.c_int), ("y", ctypes.c_void_p), ("ldy", ctypes.c_longlong),
+                ("z", ctypes.c_void_p), ("ldz", ctypes.c_longlong)]
+
+
+class MatmulBackwardArgs(ctypes.Structure):
+    _fields_ = [("precision", ctypes.c_int), ("M", ctypes.c_longlong), ("N", ctypes.c_int),
+                ("K", ctypes.c_int), ("dy", ctypes.c_void_p), ("lddy", ctypes.c_longlong),
+                ("z", ctypes.c_void_p), ("ldz", ctypes.c_longlong), ("act", ctypes.c_int),
+                ("x", ctypes.c_void_p), ("ldx", ctypes.c_longlong), ("w", ctypes.c_void_p),
+                ("ldw", ctypes.c_longlong), ("dz", ctypes.c_void_p), ("lddz", ctypes.c_longlong),
+                ("dx", ctypes.c_void_p), ("lddx", ctypes.c_longlong), ("dw", ctypes.c_void_p),
+                ("dw_precision", ctypes.c_int), ("db", ctypes.c_void_p)]
+
+
 class AdamwTensor(ctypes.Structure):
     _fields_ = [("w", ctypes.c_void_p), ("g", ctypes.c_void_p), ("m", ctypes.c_void_p),
                 ("v", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("low", ctypes.c_void_p),
@@ -186,6 +205,10 @@ _SIGS = {
     "ekya_op_groupnorm_backward_workspace": (ctypes.c_size_t, [_I, _I, _LL, _I, _I]),
     "ekya_op_groupnorm_backward": (_I, [_I, _P, _P, _I, _LL, _I, _I, _P, _P, _P, _P, _I, _P, _P, _P,
                                         _P, ctypes.c_size_t, _P]),
+    "ekya_op_matmul_workspace": (ctypes.c_size_t, [ctypes.POINTER(MatmulArgs)]),
+    "ekya_op_matmul": (_I, [ctypes.POINTER(MatmulArgs), _P, ctypes.c_size_t, _P]),
+    "ekya_op_matmul_backward_workspace": (ctypes.c_size_t, [ctypes.POINTER(MatmulBackwardArgs)]),
+    "ekya_op_matmul_backward": (_I, [ctypes.POINTER(MatmulBackwardArgs), _P, ctypes.c_size_t, _P]),
     "ekya_adamw_create": (_I, [ctypes.POINTER(_P), ctypes.POINTER(AdamwTensor), _I, _I, _I]),
     "ekya_adamw_destroy": (None, [_P]),
     "ekya_adamw_set_grads": (_I, [_P, ctypes.POINTER(_P), _I]),
@@ -782,6 +805,97 @@ def ekya_op_groupnorm_backward(dy, x, groups: int, gamma, beta, mean, rstd,
                                        _dev(rstd, f32), act, _dev(dx, x.dtype), _dev(dgamma),
                                        _dev(dbeta), _dev(ws), nbytes, _stream()))
     return dx, dgamma, dbeta
+
+
+def _matrix(t, rows: int, cols: int, dtype, name: str):
+    """(pointer, elements between rows) of a [rows, cols] view whose columns lie next to each other."""
+    if t is None:
+        return None, 0
+    _shaped(t, (rows, cols), name)
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if cols > 1 and t.stride(1) != 1 and rows > 0:
+        raise ValueError(f"{name}: the columns of a row must lie next to each other")
+    return t.data_ptr() or None, max(t.stride(0), cols) if rows <= 1 else t.stride(0)
+
+
+def _matmul_dims(x, w):
+    if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
+        raise ValueError(f"expected x [M, K] and w [N, K], got {tuple(x.shape)} and {tuple(w.shape)}")
+    return x.shape[0], w.shape[0], x.shape[1]
+
+
+def ekya_op_matmul(x, w, bias=None, act: int = EKYA_ACT_NONE, residual=None,
+                   residual_first: bool = False, keep_z: bool = False, y=None):
+    """(y, z): y = act(s) [+ residual] with s = x w^T + bias [+ residual where it comes first]; z = s
+    where kept, else None.  x [M, K], w [N, K], residual [M, N] of one type, rows any distance
+    apart; y may be the residual."""
+    torch = _torch()
+    lib = load()
+    M, N, K = _matmul_dims(x, w)
+    _on_current(x, w, bias, residual, y)
+    _shaped(bias, (N,), "bias")
+    dt = x.dtype
+    y = torch.empty(M, N, dtype=dt, device=x.device) if y is None else y
+    z = torch.empty(M, N, dtype=dt, device=x.device) if keep_z else None
+    a = MatmulArgs()
+    a.precision, a.M, a.N, a.K, a.act = _precision(x), M, N, K, act
+    a.x, a.ldx = _matrix(x, M, K, dt, "x")
+    a.w, a.ldw = _matrix(w, N, K, dt, "w")
+    a.bias = _dev(bias, torch.float32)
+    a.residual, a.ldr = _matrix(residual, M, N, dt, "residual")
+    a.residual_first = int(residual_first)
+    a.y, a.ldy = _matrix(y, M, N, dt, "y")
+    a.z, a.ldz = _matrix(z, M, N, dt, "z")
+    args = ctypes.byref(a)
+    nbytes = lib.ekya_op_matmul_workspace(args)
+    ws = _scratch(nbytes, x.device)
+    _op(lib.ekya_op_matmul(args, _dev(ws), nbytes, _stream()))
+    return y, z
+
+
+def ekya_op_matmul_backward(dy, x, w, act: int = EKYA_ACT_NONE, z=None, dw_dtype=None, dx=None,
+                            dz=None, need_dx: bool = True, need_dw: bool = True,
+                            need_db: bool = True):
+    """(dx, dw, db, dz) of ekya_op_matmul for dy [M, N]; z as it was kept (not needed without an
+    activation; dz is then dy itself and None is returned).  dw_dtype: float32 (default), or x's.
+    dz may be dy or z.  What is not needed is None."""
+    torch = _torch()
+    lib = load()
+    M, N, K = _matmul_dims(x, w)
+    _on_current(x, w, dy, z, dx, dz)
+    dt, dev = x.dtype, x.device
+    dw_dtype = torch.float32 if dw_dtype is None else dw_dtype
+    if dw_dtype not in (torch.float32, dt):
+        raise TypeError(f"dw: expected float32 or {dt}, got {dw_dtype}")
+    has_act = act != EKYA_ACT_NONE
+    if has_act and z is None:
+        raise ValueError("z is needed behind an activation")
+    if not has_act:
+        z = dz = None
+    if has_act and dz is None:
+        dz = torch.empty(M, N, dtype=dt, device=dev)
+    if not need_dx:
+        dx = None
+    elif dx is None:
+        dx = torch.empty(M, K, dtype=dt, device=dev)
+    dw = torch.empty(N, K, dtype=dw_dtype, device=dev) if need_dw else None
+    db = torch.empty(N, dtype=torch.float32, device=dev) if need_db else None
+    a = MatmulBackwardArgs()
+    a.precision, a.M, a.N, a.K, a.act = _precision(x), M, N, K, act
+    a.dy, a.lddy = _matrix(dy, M, N, dt, "dy")
+    a.z, a.ldz = _matrix(z, M, N, dt, "z")
+    a.x, a.ldx = _matrix(x, M, K, dt, "x")
+    a.w, a.ldw = _matrix(w, N, K, dt, "w")
+    a.dz, a.lddz = _matrix(dz, M, N, dt, "dz")
+    a.dx, a.lddx = _matrix(dx, M, K, dt, "dx")
+    a.dw, a.db = _dev(dw), _dev(db)
+    a.dw_precision = EKYA_FP32 if dw_dtype == torch.float32 else EKYA_BF16
+    args = ctypes.byref(a)
+    nbytes = lib.ekya_op_matmul_backward_workspace(args)
+    ws = _scratch(nbytes, dev)
+    _op(lib.ekya_op_matmul_backward(args, _dev(ws), nbytes, _stream()))
+    return dx, dw, db, dz
 
 
 class Adamw:

@@ -774,6 +774,119 @@ ekya_status ekya_op_groupnorm_backward(int precision, const void* dy, const void
 
 namespace {
 
+// A matrix in memory: rows ld elements of `size` bytes apart.
+struct Mat {
+  const void* p;
+  long long rows, cols, ld;
+  size_t size;
+  size_t span() const { return rows && cols ? ((rows - 1) * ld + cols) * size : 0; }
+};
+
+// Whether two matrices may share an element: their spans meet, and they are
+// not different columns of rows of one length.
+bool overlap(const Mat& a, const Mat& b) {
+  if (!a.span() || !b.span() || !overlap(a.p, a.span(), b.p, b.span())) return false;
+  const size_t L = a.ld * a.size;
+  if (L != b.ld * b.size) return true;
+  const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+  const size_t o = y >= x ? (y - x) % L : (L - (x - y) % L) % L;
+  return o < a.cols * a.size || o + b.cols * b.size > L;
+}
+bool same(const Mat& a, const Mat& b) { return a.p == b.p && a.ld == b.ld; }
+
+// A matrix that is there, on its elements, with rows that do not overlap and
+// at most 2^40 elements' span.
+bool mat_ok(const Mat& m) {
+  return m.p && aligned(m.p, m.size) && m.ld >= m.cols &&
+         (m.rows <= 1 || m.ld <= (1LL << 42) / m.rows);
+}
+
+bool matmul_sizes_ok(int precision, long long M, int N, int K) {
+  return valid_precision(precision) && M >= 0 && N >= 1 && K >= 1 && N <= (1 << 24) &&
+         K <= (1 << 24) && M <= (1LL << 40) / std::max(N, K);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ekya_op_matmul_workspace(const ekya_matmul_args* a) {
+  if (!a || !matmul_sizes_ok(a->precision, a->M, a->N, a->K)) return 0;
+  return ekya::matmul_workspace_floats(a->precision, a->M, a->N, a->K) * sizeof(float);
+}
+
+ekya_status ekya_op_matmul(const ekya_matmul_args* args, void* workspace, size_t workspace_bytes,
+                           void* stream) {
+  if (!args) return fail(nullptr, EKYA_ERR_INVALID_ARG, "matmul: args is null");
+  const ekya_matmul_args& a = *args;
+  if (!matmul_sizes_ok(a.precision, a.M, a.N, a.K) || !valid_act(a.act))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG, "invalid matmul sizes, precision or activation");
+  if (a.M == 0) return EKYA_OK;
+  const size_t e = ekya::dtype_size(a.precision);
+  const Mat x{a.x, a.M, a.K, a.ldx, e}, w{a.w, a.N, a.K, a.ldw, e}, y{a.y, a.M, a.N, a.ldy, e},
+      z{a.z, a.M, a.N, a.ldz, e}, r{a.residual, a.M, a.N, a.ldr, e},
+      bias{a.bias, 1, a.N, a.N, sizeof(float)};
+  if (!mat_ok(x) || !mat_ok(w) || !mat_ok(y) || (a.z && !mat_ok(z)) || (a.residual && !mat_ok(r)) ||
+      !aligned(a.bias, 4))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG, "matmul: a matrix is null, misaligned or its ld too small");
+  if (overlap(y, x) || overlap(y, w) || (a.bias && overlap(y, bias)) ||
+      (a.residual && !same(y, r) && overlap(y, r)) ||
+      (a.z && (overlap(z, x) || overlap(z, w) || overlap(z, y) || (a.residual && overlap(z, r)) ||
+               (a.bias && overlap(z, bias)))))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG, "matmul: an output overlaps another matrix");
+  const size_t need = ekya_op_matmul_workspace(args);
+  if (ekya_status s = check_workspace("matmul", workspace, workspace_bytes, need)) return s;
+  const ekya::MatmulFwd f{a.precision, a.M,   a.N,        a.K,   a.x,              a.ldx,
+                          a.w,         a.ldw, a.bias,     a.act, a.residual,       a.ldr,
+                          a.residual_first,   a.y,        a.ldy, a.z,              a.ldz};
+  return hip_status(ekya::matmul_fwd(f, (float*)workspace, (hipStream_t)stream));
+}
+
+size_t ekya_op_matmul_backward_workspace(const ekya_matmul_backward_args* a) {
+  if (!a || !matmul_sizes_ok(a->precision, a->M, a->N, a->K)) return 0;
+  return ekya::matmul_backward_workspace_floats(a->precision, a->M, a->N, a->K, a->dx, a->dw, a->db) *
+         sizeof(float);
+}
+
+ekya_status ekya_op_matmul_backward(const ekya_matmul_backward_args* args, void* workspace,
+                                    size_t workspace_bytes, void* stream) {
+  if (!args) return fail(nullptr, EKYA_ERR_INVALID_ARG, "matmul_backward: args is null");
+  const ekya_matmul_backward_args& a = *args;
+  if (!matmul_sizes_ok(a.precision, a.M, a.N, a.K) || !valid_act(a.act) ||
+      (a.dw && a.dw_precision != EKYA_FP32 && a.dw_precision != a.precision))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG, "invalid matmul_backward sizes, precision or activation");
+  const size_t e = ekya::dtype_size(a.precision), we = a.dw ? ekya::dtype_size(a.dw_precision) : 4;
+  const bool act = a.act != EKYA_ACT_NONE;
+  const Mat dy{a.dy, a.M, a.N, a.lddy, e}, z{act ? a.z : nullptr, a.M, a.N, a.ldz, e},
+      x{a.dw ? a.x : nullptr, a.M, a.K, a.ldx, e}, w{a.dx ? a.w : nullptr, a.N, a.K, a.ldw, e},
+      dz{act ? a.dz : nullptr, a.M, a.N, a.lddz, e}, dx{a.dx, a.M, a.K, a.lddx, e},
+      dw{a.dw, a.N, a.K, a.K, we}, db{a.db, 1, a.N, a.N, sizeof(float)};
+  if ((a.M > 0 && (!mat_ok(dy) || (act && (!mat_ok(z) || !mat_ok(dz))) || (a.dw && !mat_ok(x)) ||
+                   (a.dx && (!mat_ok(w) || !mat_ok(dx))))) ||
+      !aligned(a.dw, we) || !aligned(a.db, 4))
+    return fail(nullptr, EKYA_ERR_INVALID_ARG,
+                "matmul_backward: a matrix is null, misaligned or its ld too small");
+  const Mat in[] = {dy, z, x, w}, out[] = {dz, dx, dw, db};
+  for (int i = 0; i < 4; ++i) {
+    if (!out[i].p) continue;
+    for (const Mat& m : in)
+      if (m.p && overlap(out[i], m) && !(i == 0 && (same(out[i], dy) || same(out[i], z)) && same(out[i], m)))
+        return fail(nullptr, EKYA_ERR_INVALID_ARG, "matmul_backward: an output overlaps an input");
+    for (int j = 0; j < i; ++j)
+      if (out[j].p && overlap(out[i], out[j]))
+        return fail(nullptr, EKYA_ERR_INVALID_ARG, "matmul_backward: outputs overlap");
+  }
+  const size_t need = ekya_op_matmul_backward_workspace(args);
+  if (ekya_status s = check_workspace("matmul_backward", workspace, workspace_bytes, need)) return s;
+  const ekya::MatmulBwd f{a.precision, a.M,    a.N,  a.K,    a.dy, a.lddy, a.z,  a.ldz,          a.act, a.x,
+                          a.ldx,       a.w,    a.ldw, a.dz,  a.lddz, a.dx, a.lddx, a.dw, a.dw_precision, a.db};
+  return hip_status(ekya::matmul_bwd(f, (float*)workspace, (hipStream_t)stream));
+}
+
+}  // extern "C"
+
+namespace {
+
 using Range = std::pair<uintptr_t, uintptr_t>;
 
 // Whether [p, p + bytes) meets one of the ascending, disjoint ranges.

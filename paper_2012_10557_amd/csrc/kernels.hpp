@@ -392,6 +392,54 @@ hipError_t groupnorm_bwd(int dt, const void* dy, const void* x, int N, long long
                          const float* rstd, int act, void* dx, float* dgamma, float* dbeta,
                          float* ws, hipStream_t stream);
 
+// s = x w^T + bias [+ res], y = act(s) [+ res], z = s; and the gradient
+// dz = dy act'(z), dx = dz w, dw = dz^T x, db = column sums.  Elements of dt
+// (dw: fp32, or bf16 where dw_dt and dt are); N, K <= 2^24.  `ws` holds
+// *_workspace_floats floats on 16 bytes.
+struct MatmulFwd {
+  int dt;
+  long long M;
+  int N, K;
+  const void* x;
+  long long ldx;
+  const void* w;
+  long long ldw;
+  const float* bias;
+  int act;
+  const void* res;
+  long long ldr;
+  int res_first;
+  void* y;
+  long long ldy;
+  void* z;
+  long long ldz;
+};
+struct MatmulBwd {
+  int dt;
+  long long M;
+  int N, K;
+  const void* dy;
+  long long lddy;
+  const void* z;
+  long long ldz;
+  int act;
+  const void* x;
+  long long ldx;
+  const void* w;
+  long long ldw;
+  void* dz;
+  long long lddz;
+  void* dx;
+  long long lddx;
+  void* dw;
+  int dw_dt;
+  float* db;
+};
+size_t matmul_workspace_floats(int dt, long long M, int N, int K);
+hipError_t matmul_fwd(const MatmulFwd& f, float* ws, hipStream_t stream);
+size_t matmul_backward_workspace_floats(int dt, long long M, int N, int K, bool dx, bool dw, bool db);
+hipError_t matmul_bwd(const MatmulBwd& f, float* ws, hipStream_t stream);
+
 // One AdamW step over tensors whose states are fp32 (bits 32) or 8-bit codes
 // with scales (bits 8); gradients of grad_dt.  step_device: the step's number
 // is read there when the kernels run (null: `step`).

@@ -1,0 +1,639 @@
+// Matrix products with everything elementwise behind them in the same kernel,
+// and their gradients.
+//
+//   D[r][c] = sum_t A(r, t) B(c, t)
+//
+//   forward  y[m][n]:  A = w[n][k],  B = x[m][k],   t = k
+//   dx[m][k]:          A = w[n][k]^, B = dz[m][n],  t = n
+//   dw[n][k]:          A = x[m][k]^, B = dz[m][n]^, t = m
+//
+// r is the direction in which the result lies in memory, t the reduction; an
+// operand marked ^ lies in memory with t as its rows.  A block of 4 or 8 waves
+// owns a tile of D; stages of 64 bytes of the reduction per row (32 bf16, 16
+// fp32) pass through a ring in LDS, and the fragments of the next stage are
+// read into registers while the matrix cores work on this one's.
+#include <algorithm>
+
+#include "act.hpp"
+#include "kernels.hpp"
+
+namespace ekya {
+namespace {
+
+__device__ __align__(16) uint4 g_mm_zero[1];
+
+// The wave's own LDS accesses are done, then all waves meet; what waves still
+// have in flight from global memory is left in flight.
+__device__ __forceinline__ void mm_barrier() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <typename T> struct MmArgs {
+  const T *a, *b;
+  long long lda, ldb;
+  long long R, C, Tn;  // outputs along r and c, reduction length
+  const float* bias;   // [R] or null
+  const T* res;        // [C][R] or null
+  long long ldr;
+  int res_first;
+  void* y;  // [C][R]
+  long long ldy;
+  T* z;     // [C][R] or null
+  long long ldz;
+  int vec;      // bias, res, y and z allow 16-byte accesses at multiples of 16 outputs
+  float* part;  // [split][C][R] where splits > 1
+  int tiles_r, tiles_c, splits, stages;  // stages of a split
+};
+
+// ------------------------------------------------------------- epilogue
+template <typename T, int N> __device__ __forceinline__ void load_run(const T* p, float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += Elt<T>::E) {
+    Unit<T> t;
+    t.u = *reinterpret_cast<const uint4*>(p + i);
+#pragma unroll
+    for (int e = 0; e < Elt<T>::E; ++e) v[i + e] = to_f(t.e[e]);
+  }
+}
+template <typename T, int N> __device__ __forceinline__ void store_run(T* p, const float (&v)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; i += Elt<T>::E) {
+    Unit<T> t;
+#pragma unroll
+    for (int e = 0; e < Elt<T>::E; ++e) t.e[e] = from_f<T>(v[i + e]);
+    *reinterpret_cast<uint4*>(p + i) = t.u;
+  }
+}
+
+// Finishes N outputs (r .. r + N - 1, c), N a multiple of a unit; v: the sums.
+template <typename T, typename OT, int ACT, int N>
+__device__ __forceinline__ void mm_finish(const MmArgs<T>& a, long long r, long long c, float (&v)[N]) {
+  if (a.vec && r + N <= a.R) {
+    float w[N];
+    if (a.bias) {
+      load_run(a.bias + r, w);
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += w[i];
+    }
+    if (a.res) load_run(a.res + c * a.ldr + r, w);
+    if (a.res && a.res_first)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += w[i];
+    if (a.z) store_run(a.z + c * a.ldz + r, v);
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = act_fwd<ACT, T>(v[i]);
+    if (a.res && !a.res_first)
+#pragma unroll
+      for (int i = 0; i < N; ++i) v[i] += w[i];
+    store_run((OT*)a.y + c * a.ldy + r, v);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    if (r + i >= a.R) continue;
+    float s = v[i];
+    if (a.bias) s += a.bias[r + i];
+    const float w = a.res ? to_f(a.res[c * a.ldr + r + i]) : 0.f;
+    if (a.res_first) s += w;
+    if (a.z) a.z[c * a.ldz + r + i] = from_f<T>(s);
+    s = act_fwd<ACT, T>(s);
+    if (!a.res_first) s += w;
+    ((OT*)a.y)[c * a.ldy + r + i] = from_f<OT>(s);
+  }
+}
+
+// ------------------------------------------------------------- operands
+typedef short mm_v4i16 __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint2 mm_read_tr(const char* p) {
+  mm_v4i16 v = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+      (__attribute__((address_space(3))) mm_v4i16*)(__attribute__((address_space(3))) char*)p);
+  return __builtin_bit_cast(uint2, v);
+}
+
+// A wave's fragment i holds outputs 16 i + (lane mod 16) of B; of A, whose
+// lanes end up with accumulators of four consecutive outputs, outputs
+// 64 (i / 4) + 16 (f / 4) + 4 (i mod 4) + f mod 4 with f = lane mod 16: a
+// lane's accumulators of four fragments are then 16 consecutive outputs.
+//
+// LDS layout of a stage.  Rows of t-contiguous operands are 4 units of 16
+// bytes; unit u of row r is stored at u ^ f(r).  Operands with t as rows keep
+// their rows of BX outputs; unit u of row t is stored at u ^ h(t).  f and h
+// spread what 8 (16-byte reads) or 16 (8-byte reads) consecutive lanes touch
+// over all banks.
+template <typename T, int BX, bool OC, bool IS_A> struct MmOperand {
+  static constexpr int E = Elt<T>::E;
+  static constexpr int TS = 4 * E;               // reduction elements of a stage
+  static constexpr int UNITS = BX * 4;           // units of a stage
+  static constexpr int RU = OC ? BX / E : 4;     // units of a row in LDS
+  static __device__ __forceinline__ int swizzle(int row) {
+    if constexpr (!OC) return IS_A ? ((row >> 1) & 1) | ((row >> 3) & 2) : (row >> 1) & 3;
+    if constexpr (sizeof(T) == 4) return IS_A ? (row >> 2) & 3 : ((row >> 2) & 3) << 2;
+    return IS_A ? (row & 1) | ((row & 2) << 2) : (row & 3) << 1;
+  }
+  // Source of the unit stored at position q of a stage that starts at t0:
+  // its first element, or null; cnt: how many of its elements exist.
+  static __device__ __forceinline__ const T* source(const T* p, long long ld, long long X, long long x0,
+                                                    long long Tn, long long t0, int q, int& cnt) {
+    const int row = q / RU, u = (q % RU) ^ swizzle(row);
+    const long long x = OC ? x0 + u * E : x0 + row, t = OC ? t0 + row : t0 + u * E;
+    const long long left = OC ? X - x : Tn - t;
+    const bool in = OC ? t < Tn : x < X;
+    cnt = in ? (int)max(0LL, min((long long)E, left)) : 0;
+    return OC ? p + t * ld + x : p + x * ld + t;
+  }
+  // Fragments of the wave whose outputs start at `x` within the tile.
+  template <int TF> static __device__ __forceinline__ void read(const uint4* s, int x, int lane, uint4 (&f)[TF]) {
+    const int fr = lane & 15, q = lane >> 4;
+    if constexpr (!OC) {
+      const int r0 = x + (IS_A ? 16 * (fr >> 2) + (fr & 3) : fr);
+      const uint4* p = s + r0 * 4 + (q ^ swizzle(r0));
+#pragma unroll
+      for (int i = 0; i < TF; ++i) f[i] = p[(IS_A ? 64 * (i / 4) + 4 * (i % 4) : 16 * i) * 4];
+    } else if constexpr (sizeof(T) == 2) {
+      const int m = fr & 3;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int t = q * 8 + half * 4 + (fr >> 2);
+#pragma unroll
+        for (int i = 0; i < TF; ++i) {
+          const int o = x + (IS_A ? 64 * (i / 4) + 16 * m + 4 * (i % 4) : 16 * i + 4 * m);
+          const char* p = (const char*)(s + t * RU + ((o / 8) ^ swizzle(t))) + (o & 4) * 2;
+          const uint2 v = mm_read_tr(p);
+          if (half == 0) { f[i].x = v.x; f[i].y = v.y; } else { f[i].z = v.x; f[i].w = v.y; }
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < TF; ++i) {
+        const int o = x + (IS_A ? 64 * (i / 4) + 16 * (fr >> 2) + 4 * (i % 4) + (fr & 3) : 16 * i + fr);
+        uint32_t v[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int t = q * 4 + e;
+          v[e] = reinterpret_cast<const uint32_t*>(s + t * RU + ((o / 4) ^ swizzle(t)))[o & 3];
+        }
+        f[i] = make_uint4(v[0], v[1], v[2], v[3]);
+      }
+    }
+  }
+};
+
+// A unit from an address that may lie on any element.
+template <typename T> __device__ __forceinline__ uint4 load_any(const T* p, int cnt) {
+  Unit<T> t;
+  t.u = zero_unit();
+  if (cnt == Elt<T>::E) {
+    __builtin_memcpy(&t.u, p, 16);
+  } else {
+#pragma unroll
+    for (int e = 0; e < Elt<T>::E; ++e)
+      if (e < cnt) t.e[e] = p[e];
+  }
+  return t.u;
+}
+
+// Workgroups go round the 8 XCDs; each XCD gets a contiguous range of tiles,
+// and a range walks the tiles four rows at a time, so that the blocks an XCD
+// runs together share panels of both operands in its L2.
+__device__ __forceinline__ void mm_tile_of(int L, int tiles_r, int tiles_c, int& tr, int& tc) {
+  const int total = tiles_r * tiles_c;
+  const int x = L & 7, k = L >> 3;
+  const int t = x * (total >> 3) + min(x, total & 7) + k;
+  const int band = t / (4 * tiles_c), rest = t - band * 4 * tiles_c;
+  const int h = min(4, tiles_r - 4 * band);
+  tc = rest / h;
+  tr = 4 * band + rest - tc * h;
+}
+
+// BR x BC tile, WR x WC waves.  DMA: both operands are read in whole units on
+// 16 bytes (global memory to LDS directly); else through registers.
+template <typename T, typename OT, int BR, int BC, int WR, int WC, bool AOC, bool BOC, bool DMA, int ACT>
+__global__ __launch_bounds__(WR* WC * 64) void mm_kernel(MmArgs<T> a) {
+  constexpr int NW = WR * WC, NST = 4;
+  constexpr int TI = BR / WR / 16, TJ = BC / WC / 16;
+  static_assert(TI % 4 == 0, "16 outputs a lane");
+  using OpA = MmOperand<T, BR, AOC, true>;
+  using OpB = MmOperand<T, BC, BOC, false>;
+  constexpr int TS = OpA::TS, SU = OpA::UNITS + OpB::UNITS;
+  constexpr int LPS = SU / 64 / NW;  // units of a lane in a stage
+  static_assert(OpA::UNITS % 64 == 0 && SU % (64 * NW) == 0, "whole copies");
+  __shared__ uint4 smem[NST * SU];
+
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int tiles = a.tiles_r * a.tiles_c;
+  const int split = blockIdx.x / tiles;
+  int tr, tc;
+  mm_tile_of(blockIdx.x - split * tiles, a.tiles_r, a.tiles_c, tr, tc);
+  const long long r0 = (long long)tr * BR, c0 = (long long)tc * BC;
+  const long long t_begin = (long long)split * a.stages * TS;
+  const long long t_end = min(a.Tn, t_begin + (long long)a.stages * TS);
+  const int ns = (int)cdivl(t_end - t_begin, TS);
+
+  // this lane's source of copy j of stage s
+  auto source = [&](int s, int j, int& cnt) {
+    const int q = (wave + NW * j) * 64;
+    const long long t0 = t_begin + (long long)s * TS;
+    return q < OpA::UNITS ? OpA::source(a.a, a.lda, a.R, r0, t_end, t0, q + lane, cnt)
+                          : OpB::source(a.b, a.ldb, a.C, c0, t_end, t0, q - OpA::UNITS + lane, cnt);
+  };
+  const void* zero = g_mm_zero;
+  asm volatile("" : "+s"(zero));
+  auto copy = [&](int s) {  // DMA
+    uint4* slot = smem + (s % NST) * SU;
+#pragma unroll
+    for (int j = 0; j < LPS; ++j) {
+      int cnt;
+      const T* p = source(s, j, cnt);
+      dma16(cnt ? (const void*)p : zero, slot + (wave + NW * j) * 64);
+    }
+  };
+  uint4 held[LPS];  // without DMA: a stage on its way
+  auto fetch = [&](int s) {
+#pragma unroll
+    for (int j = 0; j < LPS; ++j) {
+      int cnt;
+      const T* p = source(s, j, cnt);
+      held[j] = load_any(p, cnt);
+    }
+  };
+  auto put = [&](int s) {
+    uint4* slot = smem + (s % NST) * SU;
+#pragma unroll
+    for (int j = 0; j < LPS; ++j) slot[(wave + NW * j) * 64 + lane] = held[j];
+  };
+
+  const int xr = wave / WC * (BR / WR), xc = wave % WC * (BC / WC);
+  auto frags = [&](int s, uint4 (&fa)[TI], uint4 (&fb)[TJ]) {
+    const uint4* slot = smem + (s % NST) * SU;
+    OpA::template read<TI>(slot, xr, lane, fa);
+    OpB::template read<TJ>(slot + OpA::UNITS, xc, lane, fb);
+  };
+
+  f32x4 acc[TI][TJ];
+#pragma unroll
+  for (int i = 0; i < TI; ++i)
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+
+  // Before stage s: the barrier ends every wave's reads of stage s (its
+  // fragments are in registers) and makes stage s + 1 visible.
+  if constexpr (DMA) {
+#pragma unroll
+    for (int s = 0; s < NST; ++s)
+      if (s < ns) copy(s);
+    if (ns >= NST) wait_vmcnt<LPS*(NST - 1)>(); else wait_vmcnt<0>();
+  } else {
+    fetch(0);
+    put(0);
+    if (ns > 1) {
+      fetch(1);
+      put(1);
+    }
+    if (ns > 2) fetch(2);
+  }
+  mm_barrier();
+  uint4 fa[2][TI], fb[2][TJ];
+  frags(0, fa[0], fb[0]);
+  auto step = [&](int s, uint4 (&ca)[TI], uint4 (&cb)[TJ], uint4 (&na)[TI], uint4 (&nb)[TJ]) {
+    if constexpr (DMA) {
+      if (s + 3 < ns) wait_vmcnt<LPS * 2>(); else wait_vmcnt<0>();
+    }
+    mm_barrier();
+    if constexpr (DMA) {
+      if (s + NST < ns) copy(s + NST);
+    } else {
+      if (s + 2 < ns) put(s + 2);
+      if (s + 3 < ns) fetch(s + 3);
+    }
+    if (s + 1 < ns) frags(s + 1, na, nb);
+    mma_tile(acc, ca, cb, (T*)nullptr);
+  };
+  for (int s = 0; s < ns; s += 2) {
+    step(s, fa[0], fb[0], fa[1], fb[1]);
+    if (s + 1 < ns) step(s + 1, fa[1], fb[1], fa[0], fb[0]);
+  }
+
+  const long long cl = c0 + xc + (lane & 15), rl = r0 + xr + 16 * (lane >> 4);
+#pragma unroll
+  for (int g = 0; g < TI / 4; ++g)
+#pragma unroll
+    for (int j = 0; j < TJ; ++j) {
+      const long long r = rl + 64 * g, c = cl + 16 * j;
+      if (r >= a.R || c >= a.C) continue;
+      float v[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i) v[i] = acc[4 * g + i / 4][j][i % 4];
+      if (a.splits > 1) {
+        float* p = a.part + ((long long)split * a.C + c) * a.R + r;
+        if (a.R % 4 == 0 && r + 16 <= a.R) {
+          store_run(p, v);
+        } else {
+#pragma unroll
+          for (int i = 0; i < 16; ++i)
+            if (r + i < a.R) p[i] = v[i];
+        }
+      } else {
+        mm_finish<T, OT, ACT, 16>(a, r, c, v);
+      }
+    }
+}
+
+// Adds up the splits in their order; N outputs a thread.
+template <typename T, typename OT, int ACT, int N>
+__global__ __launch_bounds__(256) void mm_reduce_kernel(MmArgs<T> a) {
+  const long long per = cdivl(a.R, N), i = (long long)blockIdx.x * 256 + threadIdx.x;
+  const long long c = i / per, r = (i - c * per) * N;
+  if (c >= a.C) return;
+  float v[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = 0.f;
+  const float* p = a.part + c * a.R + r;
+  if (a.R % 4 == 0 && r + N <= a.R) {
+    for (int s = 0; s < a.splits; ++s, p += a.C * a.R) {
+      float w[N];
+      load_run(p, w);
+#pragma unroll
+      for (int e = 0; e < N; ++e) v[e] += w[e];
+    }
+  } else {
+    for (int s = 0; s < a.splits; ++s, p += a.C * a.R)
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (r + e < a.R) v[e] += p[e];
+  }
+  mm_finish<T, OT, ACT, N>(a, r, c, v);
+}
+
+// ---------------------------------------------------------------- host side
+bool unit16(const void* p, long long ld, int dt) {
+  return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % dtype_vec(dt) == 0;
+}
+
+struct MmPlan {
+  int splits, stages;  // stages of a split
+};
+// Tiles of 128 x 128; the reduction is split until about 512 blocks run, and
+// into pieces of 8 stages at least.
+MmPlan mm_plan(long long R, long long C, long long Tn, int dt) {
+  const long long tiles = cdivl(R, 128) * cdivl(C, 128), ns = std::max(1LL, cdivl(Tn, 4 * dtype_vec(dt)));
+  const long long want = std::max(1LL, std::min(512 / std::max(1LL, tiles), ns / 8));
+  const int stages = (int)cdivl(ns, want);
+  return {(int)cdivl(ns, stages), stages};
+}
+size_t mm_part_floats(long long R, long long C, long long Tn, int dt) {
+  const MmPlan p = mm_plan(R, C, Tn, dt);
+  return p.splits > 1 ? (size_t)p.splits * R * C : 0;
+}
+
+constexpr long long MM_TILES = 1 << 21;  // tiles of a launch
+
+template <typename T, typename OT, bool AOC, bool BOC, int ACT>
+hipError_t mm_run(MmArgs<T> a, bool dma, hipStream_t st) {
+  const MmPlan p = mm_plan(a.R, a.C, a.Tn, sizeof(T) == 2 ? DT_BF16 : DT_F32);
+  a.splits = p.splits;
+  a.stages = p.stages;
+  // launches of at most MM_TILES tiles; a split product has few and goes in one
+  const long long C = a.C, tiles_r = cdivl(a.R, 128);
+  const long long cs = std::max(1LL, MM_TILES / tiles_r) * 128;
+  for (long long c = 0; c < C; c += cs) {
+    MmArgs<T> b = a;
+    b.C = std::min(cs, C - c);
+    b.b = a.b + (BOC ? c : c * a.ldb);
+    if (a.res) b.res = a.res + c * a.ldr;
+    if (a.z) b.z = a.z + c * a.ldz;
+    b.y = (OT*)a.y + c * a.ldy;
+    b.tiles_r = (int)tiles_r;
+    b.tiles_c = (int)cdivl(b.C, 128);
+    const dim3 grid((unsigned)((long long)b.tiles_r * b.tiles_c * b.splits));
+    if (dma)
+      hipLaunchKernelGGL((mm_kernel<T, OT, 128, 128, 2, 2, AOC, BOC, true, ACT>), grid, dim3(256), 0, st, b);
+    else
+      hipLaunchKernelGGL((mm_kernel<T, OT, 128, 128, 2, 2, AOC, BOC, false, ACT>), grid, dim3(256), 0, st, b);
+    EKYA_HIP(hipGetLastError());
+  }
+  if (a.splits > 1) {
+    const long long threads = a.C * cdivl(a.R, 8);
+    hipLaunchKernelGGL((mm_reduce_kernel<T, OT, ACT, 8>), dim3((unsigned)cdivl(threads, 256)), dim3(256), 0, st, a);
+    EKYA_HIP(hipGetLastError());
+  }
+  return hipSuccess;
+}
+
+template <typename T> hipError_t mm_forward(const MatmulFwd& f, float* ws, hipStream_t st) {
+  const int dt = sizeof(T) == 2 ? DT_BF16 : DT_F32, E = Elt<T>::E;
+  MmArgs<T> a{};
+  a.a = (const T*)f.w;
+  a.lda = f.ldw;
+  a.b = (const T*)f.x;
+  a.ldb = f.ldx;
+  a.R = f.N;
+  a.C = f.M;
+  a.Tn = f.K;
+  a.bias = f.bias;
+  a.res = (const T*)f.res;
+  a.ldr = f.ldr;
+  a.res_first = f.res && f.res_first;
+  a.y = f.y;
+  a.ldy = f.ldy;
+  a.z = (T*)f.z;
+  a.ldz = f.ldz;
+  a.part = ws;
+  a.vec = unit16(f.y, f.ldy, dt) && (!f.z || unit16(f.z, f.ldz, dt)) &&
+          (!f.res || unit16(f.res, f.ldr, dt)) && reinterpret_cast<uintptr_t>(f.bias) % 16 == 0;
+  const bool dma = f.K % E == 0 && unit16(f.w, f.ldw, dt) && unit16(f.x, f.ldx, dt);
+  return act_dispatch(f.act, [&](auto k) { return mm_run<T, T, false, false, k.value>(a, dma, st); });
+}
+
+// ----------------------------------------------------------------- backward
+// dz = dy act'(z), and the column sums of what is stored before its rounding.
+// A block takes a range of rows and up to 64 units of columns.
+constexpr int DZ_NT = 256;
+struct DzArgs {
+  const void *dy, *z;
+  void* dz;  // null: sums only
+  long long lddy, ldz, lddz, M;
+  int N, cu, cup, cchunks;
+  long long rows;  // of a block
+  float* part;     // [chunk][N] or null
+};
+template <typename T, int E, int ACT> __global__ __launch_bounds__(DZ_NT) void dz_kernel(DzArgs a) {
+  __shared__ float red[DZ_NT * E];
+  const int cc = blockIdx.x % a.cchunks;
+  const long long chunk = blockIdx.x / a.cchunks;
+  const int u = threadIdx.x & (a.cup - 1), rr = threadIdx.x / a.cup, rpp = DZ_NT / a.cup;
+  const int c = (cc * a.cu + u) * E;
+  const bool on = u < a.cu && c < a.N;
+  const long long r1 = min(a.M, (chunk + 1) * a.rows);
+  float s[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) s[e] = 0.f;
+  if (on)
+    for (long long r = chunk * a.rows + rr; r < r1; r += rpp) {
+      float g[E], z[E];
+      if constexpr (E > 1) {
+        load_run((const T*)a.dy + r * a.lddy + c, g);
+        if constexpr (ACT != ACT_NONE) load_run((const T*)a.z + r * a.ldz + c, z);
+      } else {
+        g[0] = to_f(((const T*)a.dy)[r * a.lddy + c]);
+        if constexpr (ACT != ACT_NONE) z[0] = to_f(((const T*)a.z)[r * a.ldz + c]);
+      }
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if constexpr (ACT != ACT_NONE) g[e] = act_bwd<ACT, T>(g[e], z[e]);
+        s[e] += g[e];
+      }
+      if (a.dz) {
+        if constexpr (E > 1)
+          store_run((T*)a.dz + r * a.lddz + c, g);
+        else
+          ((T*)a.dz)[r * a.lddz + c] = from_f<T>(g[0]);
+      }
+    }
+  if (!a.part) return;
+#pragma unroll
+  for (int e = 0; e < E; ++e) red[threadIdx.x * E + e] = s[e];
+  __syncthreads();
+  for (int h = DZ_NT / 2; h >= a.cup; h >>= 1) {
+    if ((int)threadIdx.x < h)
+#pragma unroll
+      for (int e = 0; e < E; ++e) red[threadIdx.x * E + e] += red[(threadIdx.x + h) * E + e];
+    __syncthreads();
+  }
+  if (rr == 0 && on)
+#pragma unroll
+    for (int e = 0; e < E; ++e) a.part[chunk * a.N + c + e] = red[threadIdx.x * E + e];
+}
+
+// db[c] = sum over chunks, 64 columns a block.
+__global__ __launch_bounds__(256) void db_kernel(const float* part, long long chunks, int N, float* db) {
+  __shared__ float red[256];
+  const int c = blockIdx.x * 64 + (threadIdx.x & 63);
+  float s = 0.f;
+  if (c < N)
+    for (long long k = threadIdx.x >> 6; k < chunks; k += 4) s += part[k * N + c];
+  red[threadIdx.x] = s;
+  __syncthreads();
+  if (threadIdx.x < 64 && c < N)
+    db[c] = (red[threadIdx.x] + red[threadIdx.x + 64]) + (red[threadIdx.x + 128] + red[threadIdx.x + 192]);
+}
+
+// Rows of a block: 8 a thread at least, no more than 1024 blocks' worth of
+// partial sums.
+void dz_cut(DzArgs& a, int E) {
+  const int units = cdiv(a.N, E);
+  a.cchunks = cdiv(units, 64);
+  a.cu = cdiv(units, a.cchunks);
+  a.cup = 1;
+  while (a.cup < a.cu) a.cup *= 2;
+  const long long least = 8LL * (DZ_NT / a.cup);
+  const long long want = std::max(1LL, 2048LL / a.cchunks);
+  a.rows = std::max(least, cdivl(cdivl(a.M, std::min(1024LL, want)), least) * least);
+}
+size_t db_part_floats(long long M, int N, int E) {
+  DzArgs a{};
+  a.M = M;
+  a.N = N;
+  dz_cut(a, E);
+  return (size_t)cdivl(M, a.rows) * N;
+}
+
+template <typename T, int E> hipError_t dz_run(DzArgs a, int act, float* db, hipStream_t st) {
+  dz_cut(a, E);
+  const long long chunks = cdivl(a.M, a.rows);
+  if (chunks) {
+    EKYA_HIP(act_dispatch(act, [&](auto k) {
+      hipLaunchKernelGGL((dz_kernel<T, E, k.value>), dim3((unsigned)(chunks * a.cchunks)), dim3(DZ_NT),
+                         0, st, a);
+      return hipGetLastError();
+    }));
+  }
+  if (db) {
+    hipLaunchKernelGGL(db_kernel, dim3(cdiv(a.N, 64)), dim3(256), 0, st, a.part, chunks, a.N, db);
+    EKYA_HIP(hipGetLastError());
+  }
+  return hipSuccess;
+}
+
+template <typename T> hipError_t mm_backward(const MatmulBwd& f, float* ws, hipStream_t st) {
+  const int dt = sizeof(T) == 2 ? DT_BF16 : DT_F32, E = Elt<T>::E;
+  const bool act = f.act != ACT_NONE;
+  const void* dz = act ? f.dz : f.dy;
+  const long long lddz = act ? f.lddz : f.lddy;
+  if (act || f.db) {
+    DzArgs a{};
+    a.dy = f.dy;
+    a.lddy = f.lddy;
+    a.z = f.z;
+    a.ldz = f.ldz;
+    a.dz = act ? f.dz : nullptr;
+    a.lddz = f.lddz;
+    a.M = f.M;
+    a.N = f.N;
+    a.part = f.db ? ws : nullptr;
+    const bool unit = f.N % E == 0 && unit16(f.dy, f.lddy, dt) &&
+                      (!act || (unit16(f.z, f.ldz, dt) && unit16(f.dz, f.lddz, dt)));
+    EKYA_HIP(unit ? (dz_run<T, Elt<T>::E>(a, f.act, f.db, st)) : (dz_run<T, 1>(a, f.act, f.db, st)));
+  }
+  if (f.dx && f.M > 0) {
+    MmArgs<T> a{};
+    a.a = (const T*)f.w;
+    a.lda = f.ldw;
+    a.b = (const T*)dz;
+    a.ldb = lddz;
+    a.R = f.K;
+    a.C = f.M;
+    a.Tn = f.N;
+    a.y = f.dx;
+    a.ldy = f.lddx;
+    a.part = ws;
+    a.vec = unit16(f.dx, f.lddx, dt);
+    const bool dma = f.K % E == 0 && f.N % E == 0 && unit16(f.w, f.ldw, dt) && unit16(dz, lddz, dt);
+    EKYA_HIP((mm_run<T, T, true, false, ACT_NONE>(a, dma, st)));
+  }
+  if (f.dw) {
+    MmArgs<T> a{};
+    a.a = (const T*)f.x;
+    a.lda = f.ldx;
+    a.b = (const T*)dz;
+    a.ldb = lddz;
+    a.R = f.K;
+    a.C = f.N;
+    a.Tn = f.M;
+    a.y = f.dw;
+    a.ldy = f.K;
+    a.part = ws;
+    const bool low = dt == DT_BF16 && f.dw_dt == DT_BF16;
+    a.vec = unit16(f.dw, f.K, low ? DT_BF16 : DT_F32);
+    const bool dma = f.K % E == 0 && f.N % E == 0 && unit16(f.x, f.ldx, dt) && unit16(dz, lddz, dt);
+    EKYA_HIP(low ? (mm_run<T, T, true, true, ACT_NONE>(a, dma, st))
+                 : (mm_run<T, float, true, true, ACT_NONE>(a, dma, st)));
+  }
+  return hipSuccess;
+}
+
+}  // namespace
+
+size_t matmul_workspace_floats(int dt, long long M, int N, int K) {
+  return mm_part_floats(N, M, K, dt);
+}
+
+size_t matmul_backward_workspace_floats(int dt, long long M, int N, int K, bool dx, bool dw, bool db) {
+  size_t f = 0;
+  if (db) f = std::max(db_part_floats(M, N, 1), N % dtype_vec(dt) == 0 ? db_part_floats(M, N, dtype_vec(dt)) : 0);
+  if (dx) f = std::max(f, mm_part_floats(K, M, N, dt));
+  if (dw) f = std::max(f, mm_part_floats(K, N, M, dt));
+  return f;
+}
+
+hipError_t matmul_fwd(const MatmulFwd& f, float* ws, hipStream_t st) {
+  return f.dt == DT_BF16 ? mm_forward<bf16>(f, ws, st) : mm_forward<float>(f, ws, st);
+}
+
+hipError_t matmul_bwd(const MatmulBwd& f, float* ws, hipStream_t st) {
+  return f.dt == DT_BF16 ? mm_backward<bf16>(f, ws, st) : mm_backward<float>(f, ws, st);
+}
+
+}  // namespace ekya

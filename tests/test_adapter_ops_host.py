@@ -97,3 +97,52 @@ def test_adamw_list_and_options():
     assert lib.ekya_adamw_step(None, ctypes.byref(binding.AdamwOpts(**good)), None) != binding.EKYA_OK
     lib.ekya_adamw_destroy(h)
     lib.ekya_adamw_destroy(None)
+
+
+def _matmul(ws=P, nbytes=BIG, **kw):
+    a = dict(precision=1, M=64, N=32, K=16, x=1 << 20, ldx=16, w=1 << 21, ldw=16, bias=1 << 22, act=0,
+             residual=1 << 23, ldr=32, residual_first=0, y=1 << 24, ldy=32, z=1 << 25, ldz=32)
+    a.update(kw)
+    return binding.load().ekya_op_matmul(ctypes.byref(binding.MatmulArgs(**a)), ws, nbytes, None)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(precision=5), dict(M=-1), dict(N=0), dict(K=0), dict(N=(1 << 24) + 1), dict(K=(1 << 24) + 1, ldx=1 << 25, ldw=1 << 25),
+    dict(M=1 << 36), dict(act=7), dict(x=None), dict(w=None), dict(y=None), dict(ldx=15), dict(ldw=0),
+    dict(ldy=31), dict(ldz=-32), dict(ldr=1), dict(x=(1 << 20) + 1), dict(bias=(1 << 22) + 2),
+    dict(y=(1 << 20) + 32), dict(y=(1 << 21) + 2), dict(y=1 << 25), dict(z=1 << 23),
+    dict(y=(1 << 23) + 2), dict(y=1 << 23, ldy=64), dict(y=1 << 22), dict(z=(1 << 22) - 64),
+    dict(ldx=1 << 62)])
+def test_matmul_refuses(bad):
+    assert _matmul(**bad) == binding.EKYA_ERR_INVALID_ARG
+
+
+def test_matmul_workspace_is_checked():
+    big = dict(M=8, N=8, K=1 << 16, ldx=1 << 16, ldw=1 << 16, x=1 << 30, w=1 << 32, ldr=8, ldy=8, ldz=8)
+    a = binding.MatmulArgs(precision=1, **big)
+    need = binding.load().ekya_op_matmul_workspace(ctypes.byref(a))
+    assert need > 0
+    assert _matmul(nbytes=need - 1, **big) == binding.EKYA_ERR_INVALID_ARG
+    assert _matmul(ws=None, **big) == binding.EKYA_ERR_INVALID_ARG
+    assert _matmul(ws=ctypes.c_void_p(4104), **big) == binding.EKYA_ERR_INVALID_ARG
+    assert binding.load().ekya_op_matmul_workspace(None) == 0
+    assert binding.load().ekya_op_matmul(None, P, BIG, None) == binding.EKYA_ERR_INVALID_ARG
+    assert _matmul(M=0, x=None, w=None, y=None, ws=None, nbytes=0) == binding.EKYA_OK
+
+
+def _matmul_backward(ws=P, nbytes=BIG, **kw):
+    a = dict(precision=1, M=64, N=32, K=16, dy=1 << 20, lddy=32, z=1 << 21, ldz=32, act=1, x=1 << 22, ldx=16,
+             w=1 << 23, ldw=16, dz=1 << 24, lddz=32, dx=1 << 25, lddx=16, dw=1 << 26, dw_precision=0, db=1 << 27)
+    a.update(kw)
+    return binding.load().ekya_op_matmul_backward(ctypes.byref(binding.MatmulBackwardArgs(**a)), ws, nbytes, None)
+
+
+@pytest.mark.parametrize("bad", [
+    dict(precision=2), dict(M=-5), dict(N=0), dict(K=1 << 25), dict(act=4), dict(dy=None), dict(z=None),
+    dict(dz=None), dict(x=None), dict(w=None), dict(lddy=31), dict(ldx=15), dict(lddx=15), dict(dw_precision=2),
+    dict(precision=0, dw_precision=1, ldx=16), dict(dw=(1 << 26) + 2), dict(db=(1 << 27) + 1),
+    dict(dz=(1 << 20) + 2), dict(dz=1 << 20, lddz=64), dict(dx=1 << 20), dict(dx=1 << 22), dict(dx=1 << 23),
+    dict(dx=1 << 24), dict(dw=1 << 22), dict(db=1 << 26), dict(dz=1 << 23)])
+def test_matmul_backward_refuses(bad):
+    assert _matmul_backward(**bad) == binding.EKYA_ERR_INVALID_ARG
+    assert binding.load().ekya_op_matmul_backward(None, P, BIG, None) == binding.EKYA_ERR_INVALID_ARG

@@ -1,0 +1,248 @@
+"""The matrix product with its epilogue, and its gradient, against float64.
+
+Tolerances.  U = 2^-24 is half an fp32 step.  A sum of K products in fp32 in any
+order is off by at most (K + 2) U sum |a b| (bf16 products are exact, fp32 ones
+lose another U each, bias and residual are two terms more).  Activations add
+what adapter_ref says, stored results half a step of their type.  Products of
+the backward pass are compared with products of the stored dz."""
+import pytest
+
+from tests.adapter_ref import ACTS, U, act64, act_error, half_step, slope_error, strided
+
+pytestmark = pytest.mark.gpu
+
+# M, N, K: tile edges (128, 256) and remainders, single rows and outputs, reductions shorter
+# than a stage, odd, and long enough to be split
+SIZES = [(1, 1, 1), (3, 5, 2), (1, 1024, 512), (1, 10, 513), (17, 33, 15), (16, 256, 4096),
+         (128, 128, 32), (129, 130, 64), (256, 128, 4096), (1, 8, 4096), (300, 257, 96),
+         (1001, 771, 513), (64, 64, 1000), (130, 1000, 24), (2000, 16, 2048), (5, 3000, 40),
+         (33, 520, 776), (64, 1032, 2048), (513, 264, 72), (1100, 2100, 200), (2305, 2056, 64),
+         (8, 4104, 40), (48, 24, 8200)]
+
+
+def _check(got, ref, tol, what):
+    off = (got.double() - ref).abs()
+    bad = ~(off <= tol)
+    assert not bad.any(), (what, int(bad.sum()), float((off / tol)[bad].max()))
+
+
+def _product(a, b, terms=()):
+    """a b^T + terms in float64, and the bound on its error in fp32."""
+    a, b = a.double(), b.double()
+    s, mag = a @ b.t(), a.abs() @ b.abs().t()
+    for t in terms:
+        s, mag = s + t.double(), mag + t.double().abs()
+    return s, (a.shape[1] + 2) * U * mag + 1e-37
+
+
+def _code(act):
+    return ACTS.index(act)
+
+
+class Case:
+    """Inputs whose rows are ld elements apart, `pad` more than they need, `offset` past 16 bytes."""
+
+    def __init__(self, M, N, K, dtype, pad=0, offset=0, seed=0):
+        import torch
+        gen = torch.Generator(device="cuda").manual_seed(M * 131 + N * 17 + K + seed)
+
+        def mat(rows, cols, scale):
+            t = (scale * torch.randn(rows, cols, generator=gen, device="cuda")).to(dtype)
+            return strided(t, cols + pad, offset) if pad or offset else t
+        self.x, self.w = mat(M, K, 1.0), mat(N, K, K ** -0.5)
+        self.res, self.dy, self.z = mat(M, N, 1.0), mat(M, N, 0.01), mat(M, N, 1.0)
+        self.bias = 0.1 * torch.randn(N, generator=gen, device="cuda")
+
+
+def check_forward(c, act, bias, residual, first, keep_z, y=None):
+    from paper_2012_10557_amd import binding
+    terms = ([c.bias] if bias else []) + ([c.res] if residual and first else [])
+    ref, ds = _product(c.x, c.w, terms)
+    res = c.res.double() if residual else None
+    got, z = binding.ekya_op_matmul(c.x, c.w, c.bias if bias else None, act=_code(act),
+                                    residual=c.res if residual else None, residual_first=first,
+                                    keep_z=keep_z, y=y)
+    half = half_step(got.dtype)
+    assert (z is not None) == keep_z
+    if keep_z:
+        _check(z, ref, ds + half * (ref.abs() + ds), "z")
+    out = act64(ref, act)[0]
+    err = act_error(ds, ref, act)
+    if residual and not first:
+        out, err = out + res, err + U * (out.abs() + res.abs())
+    _check(got, out, err + half * (out.abs() + err), "y")
+    return got, z
+
+
+def check_backward(c, act, dw_dtype, **kw):
+    import torch
+    from paper_2012_10557_amd import binding
+    dx, dw, db, dz = binding.ekya_op_matmul_backward(c.dy, c.x, c.w, act=_code(act),
+                                                     z=c.z if act != "none" else None,
+                                                     dw_dtype=dw_dtype, **kw)
+    g = c.dy.double() * act64(c.z.double(), act)[1]
+    dg = c.dy.double().abs() * slope_error(torch.zeros_like(g), c.z.double(), act) + 2 * U * g.abs()
+    if act == "none":
+        assert dz is None
+        dz = c.dy
+    else:
+        _check(dz, g, dg + half_step(dz.dtype) * (g.abs() + dg) + 1e-37, "dz")
+    M = g.shape[0]
+    _check(db, g.sum(0), dg.sum(0) + M * U * g.abs().sum(0) + 1e-37, "db")
+    ref, err = _product(dz, c.w.t())
+    _check(dx, ref, err + half_step(dx.dtype) * (ref.abs() + err), "dx")
+    ref, err = _product(dz.t(), c.x.t())
+    assert dw.dtype == dw_dtype
+    _check(dw, ref, err + half_step(dw.dtype) * (ref.abs() + err), "dw")
+    return dx, dw, db, dz
+
+
+@pytest.mark.parametrize("pad,offset", [(0, 0), (16, 0), (3, 1)])
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+@pytest.mark.parametrize("M,N,K", SIZES)
+def test_matmul_matches_float64(M, N, K, prec, pad, offset):
+    import torch
+    dtype = torch.float32 if prec == "f32" else torch.bfloat16
+    c = Case(M, N, K, dtype, pad, offset)
+    k = M + N + K + pad
+    act = ACTS[k % 4]
+    check_forward(c, act, bias=True, residual=k % 3 > 0, first=k % 3 == 2, keep_z=k % 2 == 0)
+    check_backward(c, act, dtype if k % 2 else torch.float32)
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+@pytest.mark.parametrize("M,N,K", [(1, 72, 256), (40, 200, 300), (200, 264, 128), (96, 72, 2048)])
+def test_every_epilogue(M, N, K, prec, act):
+    import torch
+    dtype = torch.float32 if prec == "f32" else torch.bfloat16
+    c = Case(M, N, K, dtype)
+    for bias in (False, True):
+        for residual, first in ((False, False), (True, False), (True, True)):
+            check_forward(c, act, bias, residual, first, keep_z=bias)
+    check_backward(c, act, torch.float32)
+
+
+@pytest.mark.parametrize("M", [1, 40, 300])
+def test_outputs_in_place_and_between_other_columns(M):
+    import torch
+    from paper_2012_10557_amd import binding
+    c = Case(M, 136, 256, torch.bfloat16)
+    y, z = check_forward(c, "gelu", True, True, False, True)
+    res = c.res.clone()
+    got, _ = binding.ekya_op_matmul(c.x, c.w, c.bias, act=3, residual=res, y=res)
+    assert got is res and torch.equal(res, y)
+    for pad, offset in ((8, 0), (5, 1)):  # rows of a wider buffer: the rest stays as it was
+        buf = torch.full((offset + M * (136 + pad) + 1,), 7.0, dtype=torch.bfloat16, device="cuda")
+        view = buf[offset:offset + M * (136 + pad)].view(M, 136 + pad)
+        binding.ekya_op_matmul(c.x, c.w, c.bias, act=3, residual=c.res, y=view[:, :136])
+        assert torch.equal(view[:, :136], y)
+        assert (view[:, 136:] == 7).all() and (buf[:offset] == 7).all() and buf[-1] == 7
+    dx, dw, db, dz = check_backward(c, "silu", torch.float32)
+    for name in ("dy", "z"):
+        c2 = Case(M, 136, 256, torch.bfloat16)
+        t = getattr(c2, name)
+        got = binding.ekya_op_matmul_backward(c2.dy, c2.x, c2.w, act=2, z=c2.z, dz=t)
+        assert all(torch.equal(a, b) for a, b in zip(got, (dx, dw, db, dz)))
+        assert got[3] is t
+
+
+def test_what_is_not_needed_is_left_out():
+    import torch
+    from paper_2012_10557_amd import binding
+    c = Case(70, 40, 56, torch.bfloat16)
+    full = check_backward(c, "relu", torch.bfloat16)
+    for skip in range(3):
+        need = [i != skip for i in range(3)]
+        got = binding.ekya_op_matmul_backward(c.dy, c.x, c.w, act=1, z=c.z, dw_dtype=torch.bfloat16,
+                                              need_dx=need[0], need_dw=need[1], need_db=need[2])
+        for i in range(3):
+            assert torch.equal(got[i], full[i]) if need[i] else got[i] is None
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+def test_no_rows(prec):
+    import torch
+    from paper_2012_10557_amd import binding
+    dtype = torch.float32 if prec == "f32" else torch.bfloat16
+    c = Case(4, 40, 24, dtype)
+    y, z = binding.ekya_op_matmul(c.x[:0], c.w, c.bias, keep_z=True)
+    assert y.shape == z.shape == (0, 40)
+    dx, dw, db, dz = binding.ekya_op_matmul_backward(c.dy[:0], c.x[:0], c.w, act=1, z=c.z[:0])
+    assert dx.shape == (0, 24) and not dw.any() and not db.any() and dz.shape == (0, 40)
+    assert dw.shape == (40, 24) and db.shape == (40,)
+
+
+@pytest.mark.parametrize("M", [3, 200])
+def test_a_non_finite_value_stays_in_its_row(M):
+    import torch
+    from paper_2012_10557_amd import binding
+    c = Case(M, 72, 64, torch.bfloat16)
+    clean, _ = binding.ekya_op_matmul(c.x, c.w, c.bias, act=1)
+    x = c.x.clone()
+    x[2, 5] = float("nan")
+    y, _ = binding.ekya_op_matmul(x, c.w, c.bias, act=1)
+    assert torch.isnan(y[2]).all()
+    y[2] = clean[2]
+    assert torch.equal(y, clean)
+
+
+def test_rows_past_32_bit_offsets():
+    import torch
+    M, N, K, ld = 70000, 24, 16, 40000  # 2.8e9 elements from the first row to the last
+    c = Case(M, N, K, torch.bfloat16)
+    buf = torch.empty(M * ld, dtype=torch.bfloat16, device="cuda")
+    for name, cols in (("x", K), ("res", N), ("dy", N), ("z", N)):
+        v = buf.view(M, ld)[:, 1000 * len(name):1000 * len(name) + cols]
+        v.copy_(getattr(c, name))
+        if name in ("x", "dy"):
+            setattr(c, name, v)
+    y = buf.view(M, ld)[:, 8000:8000 + N]
+    check_forward(c, "relu", True, True, False, True, y=y)
+    check_backward(c, "relu", torch.float32, dx=buf.view(M, ld)[:, 16000:16000 + K])
+
+
+def test_matmul_gradient_is_the_difference_quotient():
+    import torch
+    from paper_2012_10557_amd import binding
+    c = Case(9, 14, 11, torch.float32)
+    y, z = binding.ekya_op_matmul(c.x, c.w, c.bias, act=3, residual=c.res, residual_first=True,
+                                  keep_z=True)
+    dx, dw, db, dz = binding.ekya_op_matmul_backward(c.dy, c.x, c.w, act=3, z=z)
+
+    def loss(x, w, b, r):
+        return (act64(x @ w.t() + b + r, "gelu")[0] * c.dy.double()).sum()
+    gen = torch.Generator(device="cuda").manual_seed(5)
+    h = 1e-4  # the quotient is off by h^2 times a third derivative of order 1
+    base = [c.x.double(), c.w.double(), c.bias.double(), c.res.double()]
+    for k, grad in enumerate((dx, dw, db, dz)):
+        d = torch.randn(grad.shape, generator=gen, device="cuda").double()
+        up, down = list(base), list(base)
+        up[k], down[k] = base[k] + h * d, base[k] - h * d
+        quotient = (loss(*up) - loss(*down)) / (2 * h)
+        assert abs((grad.double() * d).sum() - quotient) <= 1e-5 * (grad.double() * d).abs().sum()
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 520, 512), (60, 64, 1024), (600, 520, 256)])
+def test_matmul_in_a_graph_repeats_the_eager_result(M, N, K):
+    import torch
+    from paper_2012_10557_amd import binding
+    c = Case(M, N, K, torch.bfloat16)
+
+    def both():
+        y, z = binding.ekya_op_matmul(c.x, c.w, c.bias, act=2, residual=c.res, keep_z=True)
+        return (y, z) + binding.ekya_op_matmul_backward(c.dy, c.x, c.w, act=2, z=z)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        both()
+    torch.cuda.current_stream().wait_stream(s)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both()
+    for i in range(3):
+        c.x.copy_(torch.randn(c.x.shape, device="cuda"))
+        eager = both()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, eager)), i
