@@ -1,5 +1,7 @@
 // Activations of the epilogues and of group norm, and their derivatives, in
-// fp32 for values stored as T.
+// fp32 for values stored as T.  Nothing here is contracted with what surrounds
+// it, so that every path of a kernel (16-byte accesses or not) gives the same
+// bits.
 #pragma once
 
 #include <type_traits>
@@ -14,34 +16,52 @@ enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2, ACT_GELU = 3 };
 // hardware's exp2 and reciprocal, off by about (|u| + 2) 2^-24, far below the
 // 2^-9 of the result's rounding.
 template <typename T> __device__ __forceinline__ float sigmoid_of(float u) {
+#pragma clang fp contract(off)
   if constexpr (sizeof(T) == 4) return 1.f / (1.f + expf(-u));
   return __builtin_amdgcn_rcpf(1.f + __expf(-u));
 }
 
 // (1 + erf(u / sqrt 2)) / 2.  fp32: by erfc, which keeps its digits where the
-// sum cancels (u far below 0); bf16: the sum, off by 2^-25 there.
-template <typename T> __device__ __forceinline__ float normal_cdf(float u) {
-  if constexpr (sizeof(T) == 4) return 0.5f * erfcf(-0.70710678f * u);
-  return 0.5f + 0.5f * erff(0.70710678f * u);
+// sum cancels (u far below 0).  bf16: 1 - erf(x) = (a1 t + .. + a5 t^5)
+// exp(-x^2), t = 1 / (1 + p x), of Abramowitz and Stegun 7.1.26, whose error of
+// 1.5e-7 is a 10000th of the result's rounding; `e` receives exp(-u^2 / 2).
+template <typename T> __device__ __forceinline__ float normal_cdf(float u, float& e) {
+#pragma clang fp contract(off)
+  if constexpr (sizeof(T) == 4) {
+    e = expf(-0.5f * u * u);
+    return 0.5f * erfcf(-0.70710678f * u);
+  }
+  e = __expf(-0.5f * u * u);
+  const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(u), 1.f));
+  float p = fmaf(t, 1.061405429f, -1.453152027f);
+  p = fmaf(t, p, 1.421413741f);
+  p = fmaf(t, p, -0.284496736f);
+  p = t * fmaf(t, p, 0.254829592f);
+  const float h = 0.5f * p * e;
+  return u < 0.f ? h : 1.f - h;
 }
 
 template <int ACT, typename T> __device__ __forceinline__ float act_fwd(float u) {
+#pragma clang fp contract(off)
   if constexpr (ACT == ACT_RELU) return relu_nan(u);
   if constexpr (ACT == ACT_SILU) return u * sigmoid_of<T>(u);
-  if constexpr (ACT == ACT_GELU) return u * normal_cdf<T>(u);
+  float e;
+  if constexpr (ACT == ACT_GELU) return u * normal_cdf<T>(u, e);
   return u;
 }
 
 // dy * act'(u).  A masked-out ReLU gradient is 0 even where dy is not finite.
 template <int ACT, typename T> __device__ __forceinline__ float act_bwd(float dy, float u) {
+#pragma clang fp contract(off)
   if constexpr (ACT == ACT_RELU) return u > 0.f ? dy : 0.f;
   if constexpr (ACT == ACT_SILU) {
     const float p = sigmoid_of<T>(u);
     return dy * (p * (1.f + u * (1.f - p)));
   }
   if constexpr (ACT == ACT_GELU) {
-    const float e = sizeof(T) == 4 ? expf(-0.5f * u * u) : __expf(-0.5f * u * u);
-    return dy * (normal_cdf<T>(u) + u * (0.39894228f * e));
+    float e;
+    const float p = normal_cdf<T>(u, e);
+    return dy * (p + u * (0.39894228f * e));
   }
   return dy;
 }

@@ -43,14 +43,17 @@ template <typename T> struct MmArgs {
   T* z;     // [C][R] or null
   long long ldz;
   int vec;      // bias, res, y and z allow 16-byte accesses at multiples of 16 outputs
-  float* part;  // [split][C][R] where splits > 1
+  float* part;  // [split][C][Rp] where splits > 1
+  long long Rp; // R up to a multiple of 4
   int tiles_r, tiles_c, splits, stages;  // stages of a split
 };
 
 // ------------------------------------------------------------- epilogue
+// N elements by 16-byte accesses (8-byte ones for four bf16).
 template <typename T, int N> __device__ __forceinline__ void load_run(const T* p, float (&v)[N]) {
+  if constexpr (N < Elt<T>::E) return load4(p, v);
 #pragma unroll
-  for (int i = 0; i < N; i += Elt<T>::E) {
+  for (int i = 0; i + Elt<T>::E <= N; i += Elt<T>::E) {
     Unit<T> t;
     t.u = *reinterpret_cast<const uint4*>(p + i);
 #pragma unroll
@@ -58,8 +61,9 @@ template <typename T, int N> __device__ __forceinline__ void load_run(const T* p
   }
 }
 template <typename T, int N> __device__ __forceinline__ void store_run(T* p, const float (&v)[N]) {
+  if constexpr (N < Elt<T>::E) return store4(p, v);
 #pragma unroll
-  for (int i = 0; i < N; i += Elt<T>::E) {
+  for (int i = 0; i + Elt<T>::E <= N; i += Elt<T>::E) {
     Unit<T> t;
 #pragma unroll
     for (int e = 0; e < Elt<T>::E; ++e) t.e[e] = from_f<T>(v[i + e]);
@@ -67,41 +71,41 @@ template <typename T, int N> __device__ __forceinline__ void store_run(T* p, con
   }
 }
 
-// Finishes N outputs (r .. r + N - 1, c), N a multiple of a unit; v: the sums.
+// Finishes N outputs (r .. r + N - 1, c) by 16-byte accesses; v: the sums,
+// bias: its N values.
 template <typename T, typename OT, int ACT, int N>
-__device__ __forceinline__ void mm_finish(const MmArgs<T>& a, long long r, long long c, float (&v)[N]) {
-  if (a.vec && r + N <= a.R) {
-    float w[N];
-    if (a.bias) {
-      load_run(a.bias + r, w);
+__device__ __forceinline__ void mm_finish(const MmArgs<T>& a, long long r, long long c, float (&v)[N],
+                                          const float (&bias)[N]) {
+  float w[N];
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += w[i];
-    }
-    if (a.res) load_run(a.res + c * a.ldr + r, w);
-    if (a.res && a.res_first)
+  for (int i = 0; i < N; ++i) v[i] += bias[i];
+  if (a.res) load_run(a.res + c * a.ldr + r, w);
+  if (a.res_first)
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += w[i];
-    if (a.z) store_run(a.z + c * a.ldz + r, v);
+    for (int i = 0; i < N; ++i) v[i] += w[i];
+  if (a.z) store_run(a.z + c * a.ldz + r, v);
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = act_fwd<ACT, T>(v[i]);
-    if (a.res && !a.res_first)
+  for (int i = 0; i < N; ++i) v[i] = act_fwd<ACT, T>(v[i]);
+  if (a.res && !a.res_first)
 #pragma unroll
-      for (int i = 0; i < N; ++i) v[i] += w[i];
-    store_run((OT*)a.y + c * a.ldy + r, v);
-    return;
-  }
+    for (int i = 0; i < N; ++i) v[i] += w[i];
+  store_run((OT*)a.y + c * a.ldy + r, v);
+}
+template <typename T, int N>
+__device__ __forceinline__ void mm_bias(const MmArgs<T>& a, long long r, float (&bias)[N]) {
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    if (r + i >= a.R) continue;
-    float s = v[i];
-    if (a.bias) s += a.bias[r + i];
-    const float w = a.res ? to_f(a.res[c * a.ldr + r + i]) : 0.f;
-    if (a.res_first) s += w;
-    if (a.z) a.z[c * a.ldz + r + i] = from_f<T>(s);
-    s = act_fwd<ACT, T>(s);
-    if (!a.res_first) s += w;
-    ((OT*)a.y)[c * a.ldy + r + i] = from_f<OT>(s);
-  }
+  for (int i = 0; i < N; ++i) bias[i] = 0.f;
+  if (a.bias) load_run(a.bias + r, bias);
+}
+template <typename T, typename OT, int ACT>
+__device__ __forceinline__ void mm_finish_one(const MmArgs<T>& a, long long r, long long c, float s) {
+  s += a.bias ? a.bias[r] : 0.f;
+  const float w = a.res ? to_f(a.res[c * a.ldr + r]) : 0.f;
+  if (a.res_first) s += w;
+  if (a.z) a.z[c * a.ldz + r] = from_f<T>(s);
+  s = act_fwd<ACT, T>(s);
+  if (!a.res_first) s += w;
+  ((OT*)a.y)[c * a.ldy + r] = from_f<OT>(s);
 }
 
 // ------------------------------------------------------------- operands
@@ -112,53 +116,44 @@ __device__ __forceinline__ uint2 mm_read_tr(const char* p) {
   return __builtin_bit_cast(uint2, v);
 }
 
-// A wave's fragment i holds outputs 16 i + (lane mod 16) of B; of A, whose
-// lanes end up with accumulators of four consecutive outputs, outputs
-// 64 (i / 4) + 16 (f / 4) + 4 (i mod 4) + f mod 4 with f = lane mod 16: a
-// lane's accumulators of four fragments are then 16 consecutive outputs.
-//
 // LDS layout of a stage.  Rows of t-contiguous operands are 4 units of 16
 // bytes; unit u of row r is stored at u ^ f(r).  Operands with t as rows keep
 // their rows of BX outputs; unit u of row t is stored at u ^ h(t).  f and h
 // spread what 8 (16-byte reads) or 16 (8-byte reads) consecutive lanes touch
 // over all banks.
-template <typename T, int BX, bool OC, bool IS_A> struct MmOperand {
+template <typename T, int BX, bool OC> struct MmOperand {
   static constexpr int E = Elt<T>::E;
   static constexpr int TS = 4 * E;               // reduction elements of a stage
   static constexpr int UNITS = BX * 4;           // units of a stage
   static constexpr int RU = OC ? BX / E : 4;     // units of a row in LDS
   static __device__ __forceinline__ int swizzle(int row) {
-    if constexpr (!OC) return IS_A ? ((row >> 1) & 1) | ((row >> 3) & 2) : (row >> 1) & 3;
-    if constexpr (sizeof(T) == 4) return IS_A ? (row >> 2) & 3 : ((row >> 2) & 3) << 2;
-    return IS_A ? (row & 1) | ((row & 2) << 2) : (row & 3) << 1;
+    if constexpr (!OC) return (row >> 1) & 3;
+    if constexpr (sizeof(T) == 4) return ((row >> 2) & 3) << 2;
+    return (row & 3) << 1;
   }
-  // Source of the unit stored at position q of a stage that starts at t0:
-  // its first element, or null; cnt: how many of its elements exist.
-  static __device__ __forceinline__ const T* source(const T* p, long long ld, long long X, long long x0,
-                                                    long long Tn, long long t0, int q, int& cnt) {
+  // Where the unit stored at position q of a stage comes from: output x (of
+  // the tile) and reduction element t (of the stage).
+  static __device__ __forceinline__ void place(int q, int& x, int& t) {
     const int row = q / RU, u = (q % RU) ^ swizzle(row);
-    const long long x = OC ? x0 + u * E : x0 + row, t = OC ? t0 + row : t0 + u * E;
-    const long long left = OC ? X - x : Tn - t;
-    const bool in = OC ? t < Tn : x < X;
-    cnt = in ? (int)max(0LL, min((long long)E, left)) : 0;
-    return OC ? p + t * ld + x : p + x * ld + t;
+    x = OC ? u * E : row;
+    t = OC ? row : u * E;
   }
-  // Fragments of the wave whose outputs start at `x` within the tile.
+  // Fragments of the wave whose outputs start at `x`, a multiple of 16, within
+  // the tile: lane f of 16 holds output 16 i + f.
   template <int TF> static __device__ __forceinline__ void read(const uint4* s, int x, int lane, uint4 (&f)[TF]) {
     const int fr = lane & 15, q = lane >> 4;
     if constexpr (!OC) {
-      const int r0 = x + (IS_A ? 16 * (fr >> 2) + (fr & 3) : fr);
-      const uint4* p = s + r0 * 4 + (q ^ swizzle(r0));
+      const uint4* p = s + (x + fr) * 4 + (q ^ swizzle(fr));
 #pragma unroll
-      for (int i = 0; i < TF; ++i) f[i] = p[(IS_A ? 64 * (i / 4) + 4 * (i % 4) : 16 * i) * 4];
+      for (int i = 0; i < TF; ++i) f[i] = p[16 * i * 4];
     } else if constexpr (sizeof(T) == 2) {
-      const int m = fr & 3;
+      // lane 4 a + m of 16 supplies outputs 4 m .. 4 m + 3 of row a of four
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
         const int t = q * 8 + half * 4 + (fr >> 2);
 #pragma unroll
         for (int i = 0; i < TF; ++i) {
-          const int o = x + (IS_A ? 64 * (i / 4) + 16 * m + 4 * (i % 4) : 16 * i + 4 * m);
+          const int o = x + 16 * i + 4 * (fr & 3);
           const char* p = (const char*)(s + t * RU + ((o / 8) ^ swizzle(t))) + (o & 4) * 2;
           const uint2 v = mm_read_tr(p);
           if (half == 0) { f[i].x = v.x; f[i].y = v.y; } else { f[i].z = v.x; f[i].w = v.y; }
@@ -167,7 +162,7 @@ template <typename T, int BX, bool OC, bool IS_A> struct MmOperand {
     } else {
 #pragma unroll
       for (int i = 0; i < TF; ++i) {
-        const int o = x + (IS_A ? 64 * (i / 4) + 16 * (fr >> 2) + 4 * (i % 4) + (fr & 3) : 16 * i + fr);
+        const int o = x + 16 * i + fr;
         uint32_t v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
@@ -213,9 +208,9 @@ template <typename T, typename OT, int BR, int BC, int WR, int WC, bool AOC, boo
 __global__ __launch_bounds__(WR* WC * 64) void mm_kernel(MmArgs<T> a) {
   constexpr int NW = WR * WC, NST = 4;
   constexpr int TI = BR / WR / 16, TJ = BC / WC / 16;
-  static_assert(TI % 4 == 0, "16 outputs a lane");
-  using OpA = MmOperand<T, BR, AOC, true>;
-  using OpB = MmOperand<T, BC, BOC, false>;
+  static_assert(TI % 4 == 0, "64 outputs of A at a time");
+  using OpA = MmOperand<T, BR, AOC>;
+  using OpB = MmOperand<T, BC, BOC>;
   constexpr int TS = OpA::TS, SU = OpA::UNITS + OpB::UNITS;
   constexpr int LPS = SU / 64 / NW;  // units of a lane in a stage
   static_assert(OpA::UNITS % 64 == 0 && SU % (64 * NW) == 0, "whole copies");
@@ -232,31 +227,66 @@ __global__ __launch_bounds__(WR* WC * 64) void mm_kernel(MmArgs<T> a) {
   const long long t_end = min(a.Tn, t_begin + (long long)a.stages * TS);
   const int ns = (int)cdivl(t_end - t_begin, TS);
 
-  // this lane's source of copy j of stage s
-  auto source = [&](int s, int j, int& cnt) {
+  // This lane's sources of the next stage.  Outputs past the end read what the
+  // last one reads: their results are not stored.
+  const T* src[LPS];
+  int whole[LPS];  // without DMA: elements of the unit that exist within its row of outputs
+#pragma unroll
+  for (int j = 0; j < LPS; ++j) {
     const int q = (wave + NW * j) * 64;
-    const long long t0 = t_begin + (long long)s * TS;
-    return q < OpA::UNITS ? OpA::source(a.a, a.lda, a.R, r0, t_end, t0, q + lane, cnt)
-                          : OpB::source(a.b, a.ldb, a.C, c0, t_end, t0, q - OpA::UNITS + lane, cnt);
+    int x, u;
+    if (q < OpA::UNITS) {
+      OpA::place(q + lane, x, u);
+      const long long last = AOC ? max(0LL, a.R - (DMA ? OpA::E : 1)) : a.R - 1;
+      const long long g = min(r0 + x, last), k = t_begin + u;
+      src[j] = AOC ? a.a + k * a.lda + g : a.a + g * a.lda + k;
+      whole[j] = AOC ? (int)min((long long)OpA::E, a.R - g) : OpA::E;
+    } else {
+      OpB::place(q - OpA::UNITS + lane, x, u);
+      const long long last = BOC ? max(0LL, a.C - (DMA ? OpB::E : 1)) : a.C - 1;
+      const long long g = min(c0 + x, last), k = t_begin + u;
+      src[j] = BOC ? a.b + k * a.ldb + g : a.b + g * a.ldb + k;
+      whole[j] = BOC ? (int)min((long long)OpB::E, a.C - g) : OpB::E;
+    }
+  }
+  const long long step_a = AOC ? TS * a.lda : TS, step_b = BOC ? TS * a.ldb : TS;
+  // reduction elements of copy j's unit that exist when `left` remain at the
+  // stage's start
+  auto there = [&](int j, int left) {
+    const int q = (wave + NW * j) * 64;
+    int x, u;
+    if (q < OpA::UNITS) {
+      OpA::place(q + lane, x, u);
+      return AOC ? (u < left ? whole[j] : 0) : max(0, min(OpA::E, left - u));
+    }
+    OpB::place(q - OpA::UNITS + lane, x, u);
+    return BOC ? (u < left ? whole[j] : 0) : max(0, min(OpB::E, left - u));
   };
   const void* zero = g_mm_zero;
   asm volatile("" : "+s"(zero));
+  auto left_at = [&](int s) { return (int)min((long long)TS, t_end - t_begin - (long long)s * TS); };
   auto copy = [&](int s) {  // DMA
     uint4* slot = smem + (s % NST) * SU;
+    const int left = left_at(s);
+    if (left == TS) {
 #pragma unroll
-    for (int j = 0; j < LPS; ++j) {
-      int cnt;
-      const T* p = source(s, j, cnt);
-      dma16(cnt ? (const void*)p : zero, slot + (wave + NW * j) * 64);
+      for (int j = 0; j < LPS; ++j) {
+        dma16(src[j], slot + (wave + NW * j) * 64);
+        src[j] += (wave + NW * j) * 64 < OpA::UNITS ? step_a : step_b;
+      }
+    } else {  // the last stage
+#pragma unroll
+      for (int j = 0; j < LPS; ++j)
+        dma16(there(j, left) ? (const void*)src[j] : zero, slot + (wave + NW * j) * 64);
     }
   };
   uint4 held[LPS];  // without DMA: a stage on its way
   auto fetch = [&](int s) {
+    const int left = left_at(s);
 #pragma unroll
     for (int j = 0; j < LPS; ++j) {
-      int cnt;
-      const T* p = source(s, j, cnt);
-      held[j] = load_any(p, cnt);
+      held[j] = load_any(src[j], left == TS ? whole[j] : there(j, left));
+      src[j] += (wave + NW * j) * 64 < OpA::UNITS ? step_a : step_b;
     }
   };
   auto put = [&](int s) {
@@ -316,29 +346,59 @@ __global__ __launch_bounds__(WR* WC * 64) void mm_kernel(MmArgs<T> a) {
     if (s + 1 < ns) step(s + 1, fa[1], fb[1], fa[0], fb[0]);
   }
 
-  const long long cl = c0 + xc + (lane & 15), rl = r0 + xr + 16 * (lane >> 4);
+  // 64 rows of the wave's tile at a time pass through its own part of LDS (no
+  // wave reads stages any more), so that a lane finishes consecutive outputs in
+  // a loop.  Without it, straight from the accumulators, the code was 10 times
+  // as long and its fetching took most of a short reduction's time (6272 x 2048
+  // x 512 with GELU: 54 us).
+  const int fr = lane & 15, q = lane >> 4;
+  const long long cw = c0 + xc;
+  const int cols = (int)min((long long)TJ * 16, a.C - cw);
+  float* part = a.part + split * a.C * a.Rp;
+  f32x4* own = reinterpret_cast<f32x4*>(smem) + wave * 16 * TJ * 16;
+  static_assert(NW * TJ * 16 * 64 * 4 <= sizeof(smem), "64 rows of every wave");
 #pragma unroll
-  for (int g = 0; g < TI / 4; ++g)
+  for (int g = 0; g < TI / 4; ++g) {
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
-    for (int j = 0; j < TJ; ++j) {
-      const long long r = rl + 64 * g, c = cl + 16 * j;
-      if (r >= a.R || c >= a.C) continue;
-      float v[16];
+    for (int j = 0; j < TJ; ++j)
 #pragma unroll
-      for (int i = 0; i < 16; ++i) v[i] = acc[4 * g + i / 4][j][i % 4];
-      if (a.splits > 1) {
-        float* p = a.part + ((long long)split * a.C + c) * a.R + r;
-        if (a.R % 4 == 0 && r + 16 <= a.R) {
-          store_run(p, v);
-        } else {
+      for (int i = 0; i < 4; ++i) own[(16 * j + fr) * 16 + ((4 * i + q) ^ fr)] = acc[4 * g + i][j];
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    const long long r0w = r0 + xr + 64 * g;
+    if (a.vec || a.splits > 1) {
+      constexpr int N = 16 / sizeof(OT), L = 64 / N;  // outputs of a lane, lanes of a column
+      const long long r = r0w + lane % L * N;
+      if (r + N <= a.R) {
+        float bias[N];
+        if (a.splits == 1) mm_bias(a, r, bias);
+        for (int k = lane / L; k < cols; k += 64 / L) {
+          float v[N];
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (r + i < a.R) p[i] = v[i];
+          for (int i = 0; i < N; i += 4) {
+            const f32x4 u = own[k * 16 + ((lane % L * N + i) / 4 ^ (k & 15))];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[i + e] = u[e];
+          }
+          if (a.splits > 1)
+            store_run(part + (cw + k) * a.Rp + r, v);
+          else
+            mm_finish<T, OT, ACT, N>(a, r, cw + k, v, bias);
         }
-      } else {
-        mm_finish<T, OT, ACT, 16>(a, r, c, v);
       }
     }
+    // rows that do not fill a lane's outputs, or all of them where accesses of
+    // 16 bytes are not possible: a lane takes one row
+    const long long r = r0w + lane, first = a.vec || a.splits > 1 ? a.R / (16 / (int)sizeof(OT)) * (16 / (int)sizeof(OT)) : 0;
+    if (r < a.R && r >= first)
+      for (int k = 0; k < cols; ++k) {
+        const float v = reinterpret_cast<const float*>(own)[(k * 16 + ((lane >> 2) ^ (k & 15))) * 4 + (lane & 3)];
+        if (a.splits > 1)
+          part[(cw + k) * a.Rp + r] = v;
+        else
+          mm_finish_one<T, OT, ACT>(a, r, cw + k, v);
+      }
+  }
 }
 
 // Adds up the splits in their order; N outputs a thread.
@@ -350,21 +410,26 @@ __global__ __launch_bounds__(256) void mm_reduce_kernel(MmArgs<T> a) {
   float v[N];
 #pragma unroll
   for (int e = 0; e < N; ++e) v[e] = 0.f;
-  const float* p = a.part + c * a.R + r;
-  if (a.R % 4 == 0 && r + N <= a.R) {
-    for (int s = 0; s < a.splits; ++s, p += a.C * a.R) {
+  const float* p = a.part + c * a.Rp + r;
+  if (a.vec && r + N <= a.R) {
+    for (int s = 0; s < a.splits; ++s, p += a.C * a.Rp) {
       float w[N];
       load_run(p, w);
 #pragma unroll
       for (int e = 0; e < N; ++e) v[e] += w[e];
     }
-  } else {
-    for (int s = 0; s < a.splits; ++s, p += a.C * a.R)
-#pragma unroll
-      for (int e = 0; e < N; ++e)
-        if (r + e < a.R) v[e] += p[e];
+    float bias[N];
+    mm_bias(a, r, bias);
+    mm_finish<T, OT, ACT, N>(a, r, c, v, bias);
+    return;
   }
-  mm_finish<T, OT, ACT, N>(a, r, c, v);
+  for (int s = 0; s < a.splits; ++s, p += a.C * a.Rp)
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (r + e < a.R) v[e] += p[e];
+#pragma unroll
+  for (int e = 0; e < N; ++e)
+    if (r + e < a.R) mm_finish_one<T, OT, ACT>(a, r + e, c, v[e]);
 }
 
 // ---------------------------------------------------------------- host side
@@ -373,31 +438,39 @@ bool unit16(const void* p, long long ld, int dt) {
 }
 
 struct MmPlan {
+  int tile;            // 256 or 128: outputs of a tile in either direction
   int splits, stages;  // stages of a split
 };
-// Tiles of 128 x 128; the reduction is split until about 512 blocks run, and
-// into pieces of 8 stages at least.
-MmPlan mm_plan(long long R, long long C, long long Tn, int dt) {
-  const long long tiles = cdivl(R, 128) * cdivl(C, 128), ns = std::max(1LL, cdivl(Tn, 4 * dtype_vec(dt)));
+// Tiles of 256 x 256 where there are enough of them for the CUs (DMA and bf16
+// only), else 128 x 128; the reduction is split until about 512 blocks run,
+// and into pieces of 8 stages at least.
+MmPlan mm_plan(long long R, long long C, long long Tn, int dt, bool dma) {
+  const long long big = cdivl(R, 256) * cdivl(C, 256);
+  const long long ns = std::max(1LL, cdivl(Tn, 4 * dtype_vec(dt)));
+  if (dma && dt == DT_BF16 && big >= 192) return {256, 1, (int)ns};
+  const long long tiles = cdivl(R, 128) * cdivl(C, 128);
   const long long want = std::max(1LL, std::min(512 / std::max(1LL, tiles), ns / 8));
   const int stages = (int)cdivl(ns, want);
-  return {(int)cdivl(ns, stages), stages};
+  return {128, (int)cdivl(ns, stages), stages};
 }
+long long round4(long long n) { return (n + 3) & ~3LL; }
 size_t mm_part_floats(long long R, long long C, long long Tn, int dt) {
-  const MmPlan p = mm_plan(R, C, Tn, dt);
-  return p.splits > 1 ? (size_t)p.splits * R * C : 0;
+  const MmPlan p = mm_plan(R, C, Tn, dt, false);
+  return p.splits > 1 ? (size_t)p.splits * C * round4(R) : 0;
 }
 
 constexpr long long MM_TILES = 1 << 21;  // tiles of a launch
+constexpr int WR256 = 2, WC256 = 4;       // waves of a 256 x 256 tile
 
 template <typename T, typename OT, bool AOC, bool BOC, int ACT>
 hipError_t mm_run(MmArgs<T> a, bool dma, hipStream_t st) {
-  const MmPlan p = mm_plan(a.R, a.C, a.Tn, sizeof(T) == 2 ? DT_BF16 : DT_F32);
+  const MmPlan p = mm_plan(a.R, a.C, a.Tn, sizeof(T) == 2 ? DT_BF16 : DT_F32, dma);
   a.splits = p.splits;
+  a.Rp = round4(a.R);
   a.stages = p.stages;
   // launches of at most MM_TILES tiles; a split product has few and goes in one
-  const long long C = a.C, tiles_r = cdivl(a.R, 128);
-  const long long cs = std::max(1LL, MM_TILES / tiles_r) * 128;
+  const long long C = a.C, tiles_r = cdivl(a.R, p.tile);
+  const long long cs = std::max(1LL, MM_TILES / tiles_r) * p.tile;
   for (long long c = 0; c < C; c += cs) {
     MmArgs<T> b = a;
     b.C = std::min(cs, C - c);
@@ -406,8 +479,15 @@ hipError_t mm_run(MmArgs<T> a, bool dma, hipStream_t st) {
     if (a.z) b.z = a.z + c * a.ldz;
     b.y = (OT*)a.y + c * a.ldy;
     b.tiles_r = (int)tiles_r;
-    b.tiles_c = (int)cdivl(b.C, 128);
+    b.tiles_c = (int)cdivl(b.C, p.tile);
     const dim3 grid((unsigned)((long long)b.tiles_r * b.tiles_c * b.splits));
+    if constexpr (sizeof(T) == 2)
+      if (p.tile == 256) {
+        hipLaunchKernelGGL((mm_kernel<T, OT, 256, 256, WR256, WC256, AOC, BOC, true, ACT>), grid,
+                           dim3(WR256 * WC256 * 64), 0, st, b);
+        EKYA_HIP(hipGetLastError());
+        continue;
+      }
     if (dma)
       hipLaunchKernelGGL((mm_kernel<T, OT, 128, 128, 2, 2, AOC, BOC, true, ACT>), grid, dim3(256), 0, st, b);
     else
@@ -507,17 +587,21 @@ template <typename T, int E, int ACT> __global__ __launch_bounds__(DZ_NT) void d
     for (int e = 0; e < E; ++e) a.part[chunk * a.N + c + e] = red[threadIdx.x * E + e];
 }
 
-// db[c] = sum over chunks, 64 columns a block.
-__global__ __launch_bounds__(256) void db_kernel(const float* part, long long chunks, int N, float* db) {
-  __shared__ float red[256];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63);
+// db[c] = sum over chunks: 32 columns a block, 32 threads a column.
+__global__ __launch_bounds__(1024) void db_kernel(const float* part, long long chunks, int N, float* db) {
+  __shared__ float red[32][33];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
   float s = 0.f;
   if (c < N)
-    for (long long k = threadIdx.x >> 6; k < chunks; k += 4) s += part[k * N + c];
-  red[threadIdx.x] = s;
+#pragma unroll 8
+    for (long long k = y; k < chunks; k += 32) s += part[k * N + c];
+  red[y][x] = s;
   __syncthreads();
-  if (threadIdx.x < 64 && c < N)
-    db[c] = (red[threadIdx.x] + red[threadIdx.x + 64]) + (red[threadIdx.x + 128] + red[threadIdx.x + 192]);
+  for (int h = 16; h > 0; h >>= 1) {
+    if (y < h) red[y][x] += red[y + h][x];
+    __syncthreads();
+  }
+  if (y == 0 && c < N) db[c] = red[0][x];
 }
 
 // Rows of a block: 8 a thread at least, no more than 1024 blocks' worth of
@@ -551,7 +635,7 @@ template <typename T, int E> hipError_t dz_run(DzArgs a, int act, float* db, hip
     }));
   }
   if (db) {
-    hipLaunchKernelGGL(db_kernel, dim3(cdiv(a.N, 64)), dim3(256), 0, st, a.part, chunks, a.N, db);
+    hipLaunchKernelGGL(db_kernel, dim3(cdiv(a.N, 32)), dim3(1024), 0, st, a.part, chunks, a.N, db);
     EKYA_HIP(hipGetLastError());
   }
   return hipSuccess;
