@@ -25,7 +25,8 @@ __device__ __align__(16) uint4 g_mm_zero[1];
 // The wave's own LDS accesses are done, then all waves meet; what waves still
 // have in flight from global memory is left in flight.
 __device__ __forceinline__ void mm_barrier() {
-  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
+  asm volatile("" ::: "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -205,7 +206,7 @@ __device__ __forceinline__ void mm_tile_of(int L, int tiles_r, int tiles_c, int&
 // BR x BC tile, WR x WC waves.  DMA: both operands are read in whole units on
 // 16 bytes (global memory to LDS directly); else through registers.
 template <typename T, typename OT, int BR, int BC, int WR, int WC, bool AOC, bool BOC, bool DMA, int ACT>
-__global__ __launch_bounds__(WR* WC * 64) void mm_kernel(MmArgs<T> a) {
+__global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
   constexpr int NW = WR * WC, NST = 4;
   constexpr int TI = BR / WR / 16, TJ = BC / WC / 16;
   static_assert(TI % 4 == 0, "64 outputs of A at a time");
@@ -265,20 +266,21 @@ __global__ __launch_bounds__(WR* WC * 64) void mm_kernel(MmArgs<T> a) {
   const void* zero = g_mm_zero;
   asm volatile("" : "+s"(zero));
   auto left_at = [&](int s) { return (int)min((long long)TS, t_end - t_begin - (long long)s * TS); };
-  auto copy = [&](int s) {  // DMA
+  auto copy_full = [&](int s) {  // DMA
     uint4* slot = smem + (s % NST) * SU;
-    const int left = left_at(s);
-    if (left == TS) {
 #pragma unroll
-      for (int j = 0; j < LPS; ++j) {
-        dma16(src[j], slot + (wave + NW * j) * 64);
-        src[j] += (wave + NW * j) * 64 < OpA::UNITS ? step_a : step_b;
-      }
-    } else {  // the last stage
-#pragma unroll
-      for (int j = 0; j < LPS; ++j)
-        dma16(there(j, left) ? (const void*)src[j] : zero, slot + (wave + NW * j) * 64);
+    for (int j = 0; j < LPS; ++j) {
+      dma16(src[j], slot + (wave + NW * j) * 64);
+      src[j] += (wave + NW * j) * 64 < OpA::UNITS ? step_a : step_b;
     }
+  };
+  auto copy = [&](int s) {
+    const int left = left_at(s);
+    if (left == TS) return copy_full(s);
+    uint4* slot = smem + (s % NST) * SU;  // the last stage
+#pragma unroll
+    for (int j = 0; j < LPS; ++j)
+      dma16(there(j, left) ? (const void*)src[j] : zero, slot + (wave + NW * j) * 64);
   };
   uint4 held[LPS];  // without DMA: a stage on its way
   auto fetch = [&](int s) {
@@ -327,6 +329,7 @@ __global__ __launch_bounds__(WR* WC * 64) void mm_kernel(MmArgs<T> a) {
   mm_barrier();
   uint4 fa[2][TI], fb[2][TJ];
   frags(0, fa[0], fb[0]);
+  // The fragments read after the last stage are not used.
   auto step = [&](int s, uint4 (&ca)[TI], uint4 (&cb)[TJ], uint4 (&na)[TI], uint4 (&nb)[TJ]) {
     if constexpr (DMA) {
       if (s + 3 < ns) wait_vmcnt<LPS * 2>(); else wait_vmcnt<0>();
@@ -338,10 +341,25 @@ __global__ __launch_bounds__(WR* WC * 64) void mm_kernel(MmArgs<T> a) {
       if (s + 2 < ns) put(s + 2);
       if (s + 3 < ns) fetch(s + 3);
     }
-    if (s + 1 < ns) frags(s + 1, na, nb);
+    frags(s + 1, na, nb);
     mma_tile(acc, ca, cb, (T*)nullptr);
   };
-  for (int s = 0; s < ns; s += 2) {
+  int s = 0;
+  if constexpr (DMA) {  // without a branch while whole stages follow
+    auto steady = [&](int s, uint4 (&ca)[TI], uint4 (&cb)[TJ], uint4 (&na)[TI], uint4 (&nb)[TJ]) {
+      wait_vmcnt<LPS * 2>();
+      mm_barrier();
+      copy_full(s + NST);
+      frags(s + 1, na, nb);
+      mma_tile(acc, ca, cb, (T*)nullptr);
+    };
+    const int full = (int)((t_end - t_begin) / TS);
+    for (; s + 1 + NST < full; s += 2) {
+      steady(s, fa[0], fb[0], fa[1], fb[1]);
+      steady(s + 1, fa[1], fb[1], fa[0], fb[0]);
+    }
+  }
+  for (; s < ns; s += 2) {
     step(s, fa[0], fb[0], fa[1], fb[1]);
     if (s + 1 < ns) step(s + 1, fa[1], fb[1], fa[0], fb[0]);
   }
@@ -359,12 +377,14 @@ __global__ __launch_bounds__(WR* WC * 64) void mm_kernel(MmArgs<T> a) {
   static_assert(NW * TJ * 16 * 64 * 4 <= sizeof(smem), "64 rows of every wave");
 #pragma unroll
   for (int g = 0; g < TI / 4; ++g) {
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the wave's own accesses, in order
+    asm volatile("" ::: "memory");
 #pragma unroll
     for (int j = 0; j < TJ; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) own[(16 * j + fr) * 16 + ((4 * i + q) ^ fr)] = acc[4 * g + i][j];
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the wave's own accesses, in order
+    asm volatile("" ::: "memory");
     const long long r0w = r0 + xr + 64 * g;
     if (a.vec || a.splits > 1) {
       constexpr int N = 16 / sizeof(OT), L = 64 / N;  // outputs of a lane, lanes of a column
