@@ -9,9 +9,10 @@
 //
 // r is the direction in which the result lies in memory, t the reduction; an
 // operand marked ^ lies in memory with t as its rows.  A block of 4 or 8 waves
-// owns a tile of D; stages of 64 bytes of the reduction per row (32 bf16, 16
-// fp32) pass through a ring in LDS, and the fragments of the next stage are
-// read into registers while the matrix cores work on this one's.
+// owns a tile of D; stages of 128 bytes of the reduction per row (64 bf16, 32
+// fp32: whole cache lines) pass through two buffers in LDS, and the fragments
+// of the next half stage are read into registers while the matrix cores work on
+// this one's.
 #include <algorithm>
 
 #include "act.hpp"
@@ -117,18 +118,18 @@ __device__ __forceinline__ uint2 mm_read_tr(const char* p) {
   return __builtin_bit_cast(uint2, v);
 }
 
-// LDS layout of a stage.  Rows of t-contiguous operands are 4 units of 16
+// LDS layout of a stage.  Rows of t-contiguous operands are 8 units of 16
 // bytes; unit u of row r is stored at u ^ f(r).  Operands with t as rows keep
 // their rows of BX outputs; unit u of row t is stored at u ^ h(t).  f and h
 // spread what 8 (16-byte reads) or 16 (8-byte reads) consecutive lanes touch
 // over all banks.
 template <typename T, int BX, bool OC> struct MmOperand {
   static constexpr int E = Elt<T>::E;
-  static constexpr int TS = 4 * E;               // reduction elements of a stage
-  static constexpr int UNITS = BX * 4;           // units of a stage
-  static constexpr int RU = OC ? BX / E : 4;     // units of a row in LDS
+  static constexpr int TS = 8 * E;               // reduction elements of a stage
+  static constexpr int UNITS = BX * 8;           // units of a stage
+  static constexpr int RU = OC ? BX / E : 8;     // units of a row in LDS
   static __device__ __forceinline__ int swizzle(int row) {
-    if constexpr (!OC) return (row >> 1) & 3;
+    if constexpr (!OC) return row & 7;
     if constexpr (sizeof(T) == 4) return ((row >> 2) & 3) << 2;
     return (row & 3) << 1;
   }
@@ -141,23 +142,25 @@ template <typename T, int BX, bool OC> struct MmOperand {
   }
   // Fragments of the wave whose outputs start at `x`, a multiple of 16, within
   // the tile: lane f of 16 holds output 16 i + f.
-  template <int TF> static __device__ __forceinline__ void read(const uint4* s, int x, int lane, uint4 (&f)[TF]) {
+  // half: of the stage.
+  template <int TF>
+  static __device__ __forceinline__ void read(const uint4* s, int half, int x, int lane, uint4 (&f)[TF]) {
     const int fr = lane & 15, q = lane >> 4;
     if constexpr (!OC) {
-      const uint4* p = s + (x + fr) * 4 + (q ^ swizzle(fr));
+      const uint4* p = s + (x + fr) * 8 + ((4 * half + q) ^ swizzle(fr));
 #pragma unroll
-      for (int i = 0; i < TF; ++i) f[i] = p[16 * i * 4];
+      for (int i = 0; i < TF; ++i) f[i] = p[16 * i * 8];
     } else if constexpr (sizeof(T) == 2) {
       // lane 4 a + m of 16 supplies outputs 4 m .. 4 m + 3 of row a of four
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int t = q * 8 + half * 4 + (fr >> 2);
+      for (int k = 0; k < 2; ++k) {
+        const int t = half * 32 + q * 8 + k * 4 + (fr >> 2);
 #pragma unroll
         for (int i = 0; i < TF; ++i) {
           const int o = x + 16 * i + 4 * (fr & 3);
           const char* p = (const char*)(s + t * RU + ((o / 8) ^ swizzle(t))) + (o & 4) * 2;
           const uint2 v = mm_read_tr(p);
-          if (half == 0) { f[i].x = v.x; f[i].y = v.y; } else { f[i].z = v.x; f[i].w = v.y; }
+          if (k == 0) { f[i].x = v.x; f[i].y = v.y; } else { f[i].z = v.x; f[i].w = v.y; }
         }
       }
     } else {
@@ -167,7 +170,7 @@ template <typename T, int BX, bool OC> struct MmOperand {
         uint32_t v[4];
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          const int t = q * 4 + e;
+          const int t = half * 16 + q * 4 + e;
           v[e] = reinterpret_cast<const uint32_t*>(s + t * RU + ((o / 4) ^ swizzle(t)))[o & 3];
         }
         f[i] = make_uint4(v[0], v[1], v[2], v[3]);
@@ -207,7 +210,7 @@ __device__ __forceinline__ void mm_tile_of(int L, int tiles_r, int tiles_c, int&
 // 16 bytes (global memory to LDS directly); else through registers.
 template <typename T, typename OT, int BR, int BC, int WR, int WC, bool AOC, bool BOC, bool DMA, int ACT>
 __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
-  constexpr int NW = WR * WC, NST = 4;
+  constexpr int NW = WR * WC, NST = 2;
   constexpr int TI = BR / WR / 16, TJ = BC / WC / 16;
   static_assert(TI % 4 == 0, "64 outputs of A at a time");
   using OpA = MmOperand<T, BR, AOC>;
@@ -298,10 +301,11 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
   };
 
   const int xr = wave / WC * (BR / WR), xc = wave % WC * (BC / WC);
-  auto frags = [&](int s, uint4 (&fa)[TI], uint4 (&fb)[TJ]) {
+  uint4 fa[2][TI], fb[2][TJ];
+  auto frags = [&](int s, int half) {
     const uint4* slot = smem + (s % NST) * SU;
-    OpA::template read<TI>(slot, xr, lane, fa);
-    OpB::template read<TJ>(slot + OpA::UNITS, xc, lane, fb);
+    OpA::template read<TI>(slot, half, xr, lane, fa[half]);
+    OpB::template read<TJ>(slot + OpA::UNITS, half, xc, lane, fb[half]);
   };
 
   f32x4 acc[TI][TJ];
@@ -310,13 +314,14 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
 #pragma unroll
     for (int j = 0; j < TJ; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
 
-  // Before stage s: the barrier ends every wave's reads of stage s (its
-  // fragments are in registers) and makes stage s + 1 visible.
+  // A stage: read its second half and multiply the first; then the barrier ends
+  // every wave's reads of it (its fragments are in registers), makes the next
+  // one visible and frees its buffer; read the next one's first half and
+  // multiply the second.
   if constexpr (DMA) {
-#pragma unroll
-    for (int s = 0; s < NST; ++s)
-      if (s < ns) copy(s);
-    if (ns >= NST) wait_vmcnt<LPS*(NST - 1)>(); else wait_vmcnt<0>();
+    if (ns > 0) copy(0);
+    if (ns > 1) copy(1);
+    if (ns > 1) wait_vmcnt<LPS>(); else wait_vmcnt<0>();
   } else {
     fetch(0);
     put(0);
@@ -327,41 +332,33 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
     if (ns > 2) fetch(2);
   }
   mm_barrier();
-  uint4 fa[2][TI], fb[2][TJ];
-  frags(0, fa[0], fb[0]);
-  // The fragments read after the last stage are not used.
-  auto step = [&](int s, uint4 (&ca)[TI], uint4 (&cb)[TJ], uint4 (&na)[TI], uint4 (&nb)[TJ]) {
-    if constexpr (DMA) {
-      if (s + 3 < ns) wait_vmcnt<LPS * 2>(); else wait_vmcnt<0>();
+  frags(0, 0);
+  int s = 0;
+  if constexpr (DMA) {  // without a branch while whole stages follow
+    const int full = (int)((t_end - t_begin) / TS);
+    for (; s + 2 < full; ++s) {
+      frags(s, 1);
+      mma_tile(acc, fa[0], fb[0], (T*)nullptr);
+      wait_vmcnt<0>();
+      mm_barrier();
+      copy_full(s);
+      frags(s + 1, 0);
+      mma_tile(acc, fa[1], fb[1], (T*)nullptr);
     }
+  }
+  for (; s < ns; ++s) {
+    frags(s, 1);
+    mma_tile(acc, fa[0], fb[0], (T*)nullptr);
+    if constexpr (DMA) wait_vmcnt<0>();
     mm_barrier();
     if constexpr (DMA) {
-      if (s + NST < ns) copy(s + NST);
+      if (s + 2 < ns) copy(s + 2);
     } else {
       if (s + 2 < ns) put(s + 2);
       if (s + 3 < ns) fetch(s + 3);
     }
-    frags(s + 1, na, nb);
-    mma_tile(acc, ca, cb, (T*)nullptr);
-  };
-  int s = 0;
-  if constexpr (DMA) {  // without a branch while whole stages follow
-    auto steady = [&](int s, uint4 (&ca)[TI], uint4 (&cb)[TJ], uint4 (&na)[TI], uint4 (&nb)[TJ]) {
-      wait_vmcnt<LPS * 2>();
-      mm_barrier();
-      copy_full(s + NST);
-      frags(s + 1, na, nb);
-      mma_tile(acc, ca, cb, (T*)nullptr);
-    };
-    const int full = (int)((t_end - t_begin) / TS);
-    for (; s + 1 + NST < full; s += 2) {
-      steady(s, fa[0], fb[0], fa[1], fb[1]);
-      steady(s + 1, fa[1], fb[1], fa[0], fb[0]);
-    }
-  }
-  for (; s < ns; s += 2) {
-    step(s, fa[0], fb[0], fa[1], fb[1]);
-    if (s + 1 < ns) step(s + 1, fa[1], fb[1], fa[0], fb[0]);
+    frags(s + 1, 0);  // after the last stage: not used
+    mma_tile(acc, fa[1], fb[1], (T*)nullptr);
   }
 
   // 64 rows of the wave's tile at a time pass through its own part of LDS (no
@@ -421,20 +418,20 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
   }
 }
 
-// Adds up the splits in their order; N outputs a thread.
+// Adds up the splits in their order; N outputs a thread (1: accesses of 16
+// bytes are not possible).
 template <typename T, typename OT, int ACT, int N>
 __global__ __launch_bounds__(256) void mm_reduce_kernel(MmArgs<T> a) {
   const long long per = cdivl(a.R, N), i = (long long)blockIdx.x * 256 + threadIdx.x;
-  const long long c = i / per, r = (i - c * per) * N;
+  const long long c = i / per, r = (i - c * per) * N, step = a.C * a.Rp;
   if (c >= a.C) return;
-  float v[N];
-#pragma unroll
-  for (int e = 0; e < N; ++e) v[e] = 0.f;
   const float* p = a.part + c * a.Rp + r;
-  if (a.vec && r + N <= a.R) {
-    for (int s = 0; s < a.splits; ++s, p += a.C * a.Rp) {
+  if constexpr (N > 1) if (r + N <= a.R) {
+    float v[N] = {};
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
       float w[N];
-      load_run(p, w);
+      load_run(p + s * step, w);
 #pragma unroll
       for (int e = 0; e < N; ++e) v[e] += w[e];
     }
@@ -443,13 +440,12 @@ __global__ __launch_bounds__(256) void mm_reduce_kernel(MmArgs<T> a) {
     mm_finish<T, OT, ACT, N>(a, r, c, v, bias);
     return;
   }
-  for (int s = 0; s < a.splits; ++s, p += a.C * a.Rp)
-#pragma unroll
-    for (int e = 0; e < N; ++e)
-      if (r + e < a.R) v[e] += p[e];
-#pragma unroll
-  for (int e = 0; e < N; ++e)
-    if (r + e < a.R) mm_finish_one<T, OT, ACT>(a, r + e, c, v[e]);
+  for (int e = 0; e < N && r + e < a.R; ++e) {
+    float v = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) v += p[s * step + e];
+    mm_finish_one<T, OT, ACT>(a, r + e, c, v);
+  }
 }
 
 // ---------------------------------------------------------------- host side
@@ -458,20 +454,34 @@ bool unit16(const void* p, long long ld, int dt) {
 }
 
 struct MmPlan {
-  int tile;            // 256 or 128: outputs of a tile in either direction
+  int tile;            // outputs of a tile in either direction
   int splits, stages;  // stages of a split
 };
-// Tiles of 256 x 256 where there are enough of them for the CUs (DMA and bf16
-// only), else 128 x 128; the reduction is split until about 512 blocks run,
-// and into pieces of 8 stages at least.
+// Which tile, and into how many parts the reduction is split.
+//
+// 256 x 256 (bf16 with DMA only) takes about 10 us and 1.58 us a stage for every
+// round of 256 tiles, one a CU; 128 x 128 about 5 us and 2.3 us and 0.46 us a
+// stage for every 256 tiles, two at a time on a CU, so that no round is waited
+// for.  Measured, 256 against 128: 8192^3 826 and 962 us, 4096^3 114 and 123,
+// 6272 x 2048 x 512 (200 tiles of 256) 23.2 and 25.2, 25088 x 1024 x 256 30.4 and
+// 31.1, 2048^3 (64 tiles of 256) 53.6 and 27.4.
+//
+// With less than 192 tiles of 128 most CUs hold one block or none: 64 x 64, and
+// the reduction split until 512 blocks run, a part 16 stages long at least (6
+// in fp32, whose stages take longer).  128 against 64: 1000^3 14.8 and 9.2 us,
+// 512^3 10.3 and 6.0, but with 256 tiles of 128 2048^3 27.4 and 28.0; parts of
+// 32, 16 and 8 stages: 1024 x 512 x 4096 21.6, 17.5 and 19.2.
 MmPlan mm_plan(long long R, long long C, long long Tn, int dt, bool dma) {
-  const long long big = cdivl(R, 256) * cdivl(C, 256);
-  const long long ns = std::max(1LL, cdivl(Tn, 4 * dtype_vec(dt)));
-  if (dma && dt == DT_BF16 && big >= 192) return {256, 1, (int)ns};
-  const long long tiles = cdivl(R, 128) * cdivl(C, 128);
-  const long long want = std::max(1LL, std::min(512 / std::max(1LL, tiles), ns / 8));
+  const long long ns = std::max(1LL, cdivl(Tn, 8 * dtype_vec(dt)));
+  const long long t256 = cdivl(R, 256) * cdivl(C, 256), t128 = cdivl(R, 128) * cdivl(C, 128);
+  if (dma && dt == DT_BF16 && t256 >= 192 &&
+      cdivl(t256, 256) * (10 + 1.58 * ns) <= 5 + t128 / 256. * (2.3 + 0.46 * ns))
+    return {256, 1, (int)ns};
+  if (t128 >= 192) return {128, 1, (int)ns};
+  const long long t64 = std::max(1LL, cdivl(R, 64) * cdivl(C, 64));
+  const long long want = std::max(1LL, std::min(512 / t64, ns / (dt == DT_BF16 ? 16 : 6)));
   const int stages = (int)cdivl(ns, want);
-  return {128, (int)cdivl(ns, stages), stages};
+  return {64, (int)cdivl(ns, stages), stages};
 }
 long long round4(long long n) { return (n + 3) & ~3LL; }
 size_t mm_part_floats(long long R, long long C, long long Tn, int dt) {
@@ -480,7 +490,6 @@ size_t mm_part_floats(long long R, long long C, long long Tn, int dt) {
 }
 
 constexpr long long MM_TILES = 1 << 21;  // tiles of a launch
-constexpr int WR256 = 2, WC256 = 4;       // waves of a 256 x 256 tile
 
 template <typename T, typename OT, bool AOC, bool BOC, int ACT>
 hipError_t mm_run(MmArgs<T> a, bool dma, hipStream_t st) {
@@ -501,22 +510,29 @@ hipError_t mm_run(MmArgs<T> a, bool dma, hipStream_t st) {
     b.tiles_r = (int)tiles_r;
     b.tiles_c = (int)cdivl(b.C, p.tile);
     const dim3 grid((unsigned)((long long)b.tiles_r * b.tiles_c * b.splits));
+    auto go = [&](auto tile, auto wr, auto wc, auto direct) {
+      hipLaunchKernelGGL((mm_kernel<T, OT, tile.value, tile.value, wr.value, wc.value, AOC, BOC, direct.value, ACT>),
+                         grid, dim3(wr.value * wc.value * 64), 0, st, b);
+    };
+    using std::integral_constant;
+    using I1 = integral_constant<int, 1>;
+    using I2 = integral_constant<int, 2>;
+    using I4 = integral_constant<int, 4>;
     if constexpr (sizeof(T) == 2)
-      if (p.tile == 256) {
-        hipLaunchKernelGGL((mm_kernel<T, OT, 256, 256, WR256, WC256, AOC, BOC, true, ACT>), grid,
-                           dim3(WR256 * WC256 * 64), 0, st, b);
-        EKYA_HIP(hipGetLastError());
-        continue;
-      }
-    if (dma)
-      hipLaunchKernelGGL((mm_kernel<T, OT, 128, 128, 2, 2, AOC, BOC, true, ACT>), grid, dim3(256), 0, st, b);
-    else
-      hipLaunchKernelGGL((mm_kernel<T, OT, 128, 128, 2, 2, AOC, BOC, false, ACT>), grid, dim3(256), 0, st, b);
+      if (p.tile == 256) go(integral_constant<int, 256>{}, I2{}, I4{}, std::true_type{});
+    if (p.tile == 128 && dma) go(integral_constant<int, 128>{}, I2{}, I2{}, std::true_type{});
+    if (p.tile == 128 && !dma) go(integral_constant<int, 128>{}, I2{}, I2{}, std::false_type{});
+    if (p.tile == 64 && dma) go(integral_constant<int, 64>{}, I1{}, I4{}, std::true_type{});
+    if (p.tile == 64 && !dma) go(integral_constant<int, 64>{}, I1{}, I4{}, std::false_type{});
     EKYA_HIP(hipGetLastError());
   }
   if (a.splits > 1) {
-    const long long threads = a.C * cdivl(a.R, 8);
-    hipLaunchKernelGGL((mm_reduce_kernel<T, OT, ACT, 8>), dim3((unsigned)cdivl(threads, 256)), dim3(256), 0, st, a);
+    const long long threads = a.C * cdivl(a.R, a.vec ? 16 / sizeof(T) : 1);
+    const dim3 grid((unsigned)cdivl(threads, 256));
+    if (a.vec)
+      hipLaunchKernelGGL((mm_reduce_kernel<T, OT, ACT, 16 / sizeof(T)>), grid, dim3(256), 0, st, a);
+    else
+      hipLaunchKernelGGL((mm_reduce_kernel<T, OT, ACT, 1>), grid, dim3(256), 0, st, a);
     EKYA_HIP(hipGetLastError());
   }
   return hipSuccess;
