@@ -74,23 +74,21 @@ template <typename T, int N> __device__ __forceinline__ void store_run(T* p, con
 }
 
 // Finishes N outputs (r .. r + N - 1, c) by 16-byte accesses; v: the sums,
-// bias: its N values.
+// bias and res: their N values (res: where there is one).
 template <typename T, typename OT, int ACT, int N>
 __device__ __forceinline__ void mm_finish(const MmArgs<T>& a, long long r, long long c, float (&v)[N],
-                                          const float (&bias)[N]) {
-  float w[N];
+                                          const float (&bias)[N], const float (&res)[N]) {
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] += bias[i];
-  if (a.res) load_run(a.res + c * a.ldr + r, w);
   if (a.res_first)
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += w[i];
+    for (int i = 0; i < N; ++i) v[i] += res[i];
   if (a.z) store_run(a.z + c * a.ldz + r, v);
 #pragma unroll
   for (int i = 0; i < N; ++i) v[i] = act_fwd<ACT, T>(v[i]);
   if (a.res && !a.res_first)
 #pragma unroll
-    for (int i = 0; i < N; ++i) v[i] += w[i];
+    for (int i = 0; i < N; ++i) v[i] += res[i];
   store_run((OT*)a.y + c * a.ldy + r, v);
 }
 template <typename T, int N>
@@ -385,22 +383,33 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
     const long long r0w = r0 + xr + 64 * g;
     if (a.vec || a.splits > 1) {
       constexpr int N = 16 / sizeof(OT), L = 64 / N;  // outputs of a lane, lanes of a column
+      constexpr int P = 64 / L, U = TJ * 16 / P < 4 ? TJ * 16 / P : 4;  // columns at once, steps in flight
       const long long r = r0w + lane % L * N;
       if (r + N <= a.R) {
         float bias[N];
         if (a.splits == 1) mm_bias(a, r, bias);
-        for (int k = lane / L; k < cols; k += 64 / L) {
-          float v[N];
+        const bool res = a.res && a.splits == 1;
+        for (int k0 = lane / L; k0 < cols; k0 += P * U) {
+          float w[U][N];  // the residual of all steps is on its way before the first is needed
+          if (res)
 #pragma unroll
-          for (int i = 0; i < N; i += 4) {
-            const f32x4 u = own[k * 16 + ((lane % L * N + i) / 4 ^ (k & 15))];
+            for (int u = 0; u < U; ++u) load_run(a.res + (cw + min(k0 + u * P, cols - 1)) * a.ldr + r, w[u]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[i + e] = u[e];
+          for (int u = 0; u < U; ++u) {
+            const int k = k0 + u * P;
+            if (k >= cols) break;
+            float v[N];
+#pragma unroll
+            for (int i = 0; i < N; i += 4) {
+              const f32x4 x = own[k * 16 + ((lane % L * N + i) / 4 ^ (k & 15))];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) v[i + e] = x[e];
+            }
+            if (a.splits > 1)
+              store_run(part + (cw + k) * a.Rp + r, v);
+            else
+              mm_finish<T, OT, ACT, N>(a, r, cw + k, v, bias, w[u]);
           }
-          if (a.splits > 1)
-            store_run(part + (cw + k) * a.Rp + r, v);
-          else
-            mm_finish<T, OT, ACT, N>(a, r, cw + k, v, bias);
         }
       }
     }
@@ -435,9 +444,10 @@ __global__ __launch_bounds__(256) void mm_reduce_kernel(MmArgs<T> a) {
 #pragma unroll
       for (int e = 0; e < N; ++e) v[e] += w[e];
     }
-    float bias[N];
+    float bias[N], res[N];
     mm_bias(a, r, bias);
-    mm_finish<T, OT, ACT, N>(a, r, c, v, bias);
+    if (a.res) load_run(a.res + c * a.ldr + r, res);
+    mm_finish<T, OT, ACT, N>(a, r, c, v, bias, res);
     return;
   }
   for (int e = 0; e < N && r + e < a.R; ++e) {
