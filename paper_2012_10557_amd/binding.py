@@ -734,34 +734,48 @@ def ekya_op_resize(frames, r: int):
 # ----------------------------------------------- adapter-training operators
 # Asynchronous on the current stream.  Scratch comes from torch's allocator,
 # which hands it out again in that stream's order; a graph's own calls draw on
-# the graph's pool.
-def _on_current(x, *others):
-    """x's device must be the current one, and the other tensors' (None: absent)."""
-    torch = _torch()
-    if not x.is_cuda or x.device.index != torch.cuda.current_device():
+# the graph's pool.  The smallest calls take a few microseconds on the GPU, so
+# the checks here are kept to a few as well.
+def _on_current(x, *others) -> int:
+    """x's device, which must be the current GPU and the other tensors' (None: absent)."""
+    d = x.get_device()
+    if d < 0 or d != _torch().cuda.current_device():
         raise ValueError("tensors must live on the current GPU")
     for t in others:
-        if t is not None and t.device != x.device:
+        if t is not None and t.get_device() != d:
             raise ValueError("tensors must live on one GPU")
+    return d
+
+
+def _raw_stream(device: int) -> int:
+    return _torch()._C._cuda_getCurrentRawStream(device)
 
 
 def _scratch(nbytes: int, device):
     return _torch().empty(nbytes, dtype=_torch().uint8, device=device) if nbytes else None
 
 
-def _shaped(t, shape, name: str):
-    if t is not None and tuple(t.shape) != tuple(shape):
+def _ptr(t, shape, dtype, name: str):
+    """The address of a contiguous tensor (None: absent)."""
+    if t is None:
+        return None
+    if t.shape != shape:
         raise ValueError(f"{name}: expected shape {tuple(shape)}, got {tuple(t.shape)}")
-    return t
+    if t.dtype != dtype:
+        raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
+    if not t.is_contiguous():
+        raise ValueError(f"{name}: tensor must be contiguous")
+    return t.data_ptr()
 
 
 def _groupnorm_dims(x):
     if x.dim() < 2:
         raise ValueError("group norm needs [N, ..., C]")
+    N, *mid, C = x.shape
     hw = 1
-    for n in x.shape[1:-1]:
+    for n in mid:
         hw *= n
-    return x.shape[0], hw, x.shape[-1]
+    return N, hw, C
 
 
 def ekya_op_groupnorm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5,
@@ -770,17 +784,17 @@ def ekya_op_groupnorm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5,
     torch = _torch()
     lib = load()
     N, HW, C = _groupnorm_dims(x)
-    _on_current(x, gamma, beta, y)
-    _shaped(gamma, (C,), "gamma"), _shaped(beta, (C,), "beta"), _shaped(y, x.shape, "y")
-    prec, f32 = _precision(x), torch.float32
-    y = torch.empty_like(x) if y is None else y
-    stats = torch.empty(2, N, max(groups, 0), dtype=f32, device=x.device)
-    mean, rstd = stats[0], stats[1]
+    d = _on_current(x, gamma, beta, y)
+    prec, dt, f32, dev, shape = _precision(x), x.dtype, torch.float32, x.device, x.shape
+    y = torch.empty(shape, dtype=dt, device=dev) if y is None else y
+    mean = torch.empty((N, max(groups, 0)), dtype=f32, device=dev)
+    rstd = torch.empty((N, max(groups, 0)), dtype=f32, device=dev)
     nbytes = lib.ekya_op_groupnorm_workspace(prec, N, HW, C, groups)
-    ws = _scratch(nbytes, x.device)
-    _op(lib.ekya_op_groupnorm(prec, _dev(x), N, HW, C, groups, _dev(gamma, f32), _dev(beta, f32), eps,
-                              act, _dev(y, x.dtype), _dev(mean), _dev(rstd), _dev(ws), nbytes,
-                              _stream()))
+    ws = _scratch(nbytes, dev)
+    _op(lib.ekya_op_groupnorm(prec, _ptr(x, shape, dt, "x"), N, HW, C, groups,
+                              _ptr(gamma, (C,), f32, "gamma"), _ptr(beta, (C,), f32, "beta"), eps, act,
+                              _ptr(y, shape, dt, "y"), mean.data_ptr(), rstd.data_ptr(),
+                              ws.data_ptr() if nbytes else None, nbytes, _raw_stream(d)))
     return y, mean, rstd
 
 
@@ -790,39 +804,41 @@ def ekya_op_groupnorm_backward(dy, x, groups: int, gamma, beta, mean, rstd,
     torch = _torch()
     lib = load()
     N, HW, C = _groupnorm_dims(x)
-    _on_current(x, dy, gamma, beta, mean, rstd, dx)
-    _shaped(dy, x.shape, "dy"), _shaped(gamma, (C,), "gamma"), _shaped(beta, (C,), "beta")
-    _shaped(mean, (N, groups), "mean"), _shaped(rstd, (N, groups), "rstd")
-    _shaped(dx, x.shape, "dx")
-    prec, f32 = _precision(x), torch.float32
-    dx = torch.empty_like(x) if dx is None else dx
-    grads = torch.empty(2, C, dtype=f32, device=x.device)
-    dgamma, dbeta = grads[0], grads[1]
+    d = _on_current(x, dy, gamma, beta, mean, rstd, dx)
+    prec, dt, f32, dev, shape = _precision(x), x.dtype, torch.float32, x.device, x.shape
+    dx = torch.empty(shape, dtype=dt, device=dev) if dx is None else dx
+    dgamma = torch.empty(C, dtype=f32, device=dev)
+    dbeta = torch.empty(C, dtype=f32, device=dev)
     nbytes = lib.ekya_op_groupnorm_backward_workspace(prec, N, HW, C, groups)
-    ws = _scratch(nbytes, x.device)
-    _op(lib.ekya_op_groupnorm_backward(prec, _dev(dy, x.dtype), _dev(x), N, HW, C, groups,
-                                       _dev(gamma, f32), _dev(beta, f32), _dev(mean, f32),
-                                       _dev(rstd, f32), act, _dev(dx, x.dtype), _dev(dgamma),
-                                       _dev(dbeta), _dev(ws), nbytes, _stream()))
+    ws = _scratch(nbytes, dev)
+    _op(lib.ekya_op_groupnorm_backward(
+        prec, _ptr(dy, shape, dt, "dy"), _ptr(x, shape, dt, "x"), N, HW, C, groups,
+        _ptr(gamma, (C,), f32, "gamma"), _ptr(beta, (C,), f32, "beta"),
+        _ptr(mean, (N, groups), f32, "mean"), _ptr(rstd, (N, groups), f32, "rstd"), act,
+        _ptr(dx, shape, dt, "dx"), dgamma.data_ptr(), dbeta.data_ptr(),
+        ws.data_ptr() if nbytes else None, nbytes, _raw_stream(d)))
     return dx, dgamma, dbeta
 
 
 def _matrix(t, rows: int, cols: int, dtype, name: str):
-    """(pointer, elements between rows) of a [rows, cols] view whose columns lie next to each other."""
+    """(address, elements between rows) of a [rows, cols] view whose columns lie next to each other."""
     if t is None:
         return None, 0
-    _shaped(t, (rows, cols), name)
+    if t.shape != (rows, cols):
+        raise ValueError(f"{name}: expected shape {(rows, cols)}, got {tuple(t.shape)}")
     if t.dtype != dtype:
         raise TypeError(f"{name}: expected {dtype}, got {t.dtype}")
-    if cols > 1 and t.stride(1) != 1 and rows > 0:
+    ld, step = t.stride()
+    if step != 1 and cols > 1 and rows > 0:
         raise ValueError(f"{name}: the columns of a row must lie next to each other")
-    return t.data_ptr() or None, max(t.stride(0), cols) if rows <= 1 else t.stride(0)
+    return t.data_ptr(), max(ld, cols) if rows <= 1 else ld
 
 
 def _matmul_dims(x, w):
     if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
         raise ValueError(f"expected x [M, K] and w [N, K], got {tuple(x.shape)} and {tuple(w.shape)}")
-    return x.shape[0], w.shape[0], x.shape[1]
+    M, K = x.shape
+    return M, w.shape[0], K
 
 
 def ekya_op_matmul(x, w, bias=None, act: int = EKYA_ACT_NONE, residual=None,
@@ -833,24 +849,17 @@ def ekya_op_matmul(x, w, bias=None, act: int = EKYA_ACT_NONE, residual=None,
     torch = _torch()
     lib = load()
     M, N, K = _matmul_dims(x, w)
-    _on_current(x, w, bias, residual, y)
-    _shaped(bias, (N,), "bias")
-    dt = x.dtype
-    y = torch.empty(M, N, dtype=dt, device=x.device) if y is None else y
-    z = torch.empty(M, N, dtype=dt, device=x.device) if keep_z else None
-    a = MatmulArgs()
-    a.precision, a.M, a.N, a.K, a.act = _precision(x), M, N, K, act
-    a.x, a.ldx = _matrix(x, M, K, dt, "x")
-    a.w, a.ldw = _matrix(w, N, K, dt, "w")
-    a.bias = _dev(bias, torch.float32)
-    a.residual, a.ldr = _matrix(residual, M, N, dt, "residual")
-    a.residual_first = int(residual_first)
-    a.y, a.ldy = _matrix(y, M, N, dt, "y")
-    a.z, a.ldz = _matrix(z, M, N, dt, "z")
+    d = _on_current(x, w, bias, residual, y)
+    dt, dev = x.dtype, x.device
+    y = torch.empty((M, N), dtype=dt, device=dev) if y is None else y
+    z = torch.empty((M, N), dtype=dt, device=dev) if keep_z else None
+    a = MatmulArgs(_precision(x), M, N, K, *_matrix(x, M, K, dt, "x"), *_matrix(w, N, K, dt, "w"),
+                   _ptr(bias, (N,), torch.float32, "bias"), act, *_matrix(residual, M, N, dt, "residual"),
+                   residual_first, *_matrix(y, M, N, dt, "y"), *_matrix(z, M, N, dt, "z"))
     args = ctypes.byref(a)
     nbytes = lib.ekya_op_matmul_workspace(args)
-    ws = _scratch(nbytes, x.device)
-    _op(lib.ekya_op_matmul(args, _dev(ws), nbytes, _stream()))
+    ws = _scratch(nbytes, dev)
+    _op(lib.ekya_op_matmul(args, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(d)))
     return y, z
 
 
@@ -863,38 +872,32 @@ def ekya_op_matmul_backward(dy, x, w, act: int = EKYA_ACT_NONE, z=None, dw_dtype
     torch = _torch()
     lib = load()
     M, N, K = _matmul_dims(x, w)
-    _on_current(x, w, dy, z, dx, dz)
-    dt, dev = x.dtype, x.device
-    dw_dtype = torch.float32 if dw_dtype is None else dw_dtype
-    if dw_dtype not in (torch.float32, dt):
+    d = _on_current(x, w, dy, z, dx, dz)
+    dt, dev, f32 = x.dtype, x.device, torch.float32
+    dw_dtype = f32 if dw_dtype is None else dw_dtype
+    if dw_dtype not in (f32, dt):
         raise TypeError(f"dw: expected float32 or {dt}, got {dw_dtype}")
-    has_act = act != EKYA_ACT_NONE
-    if has_act and z is None:
-        raise ValueError("z is needed behind an activation")
-    if not has_act:
+    if act == EKYA_ACT_NONE:
         z = dz = None
-    if has_act and dz is None:
-        dz = torch.empty(M, N, dtype=dt, device=dev)
+    elif z is None:
+        raise ValueError("z is needed behind an activation")
+    elif dz is None:
+        dz = torch.empty((M, N), dtype=dt, device=dev)
     if not need_dx:
         dx = None
     elif dx is None:
-        dx = torch.empty(M, K, dtype=dt, device=dev)
-    dw = torch.empty(N, K, dtype=dw_dtype, device=dev) if need_dw else None
-    db = torch.empty(N, dtype=torch.float32, device=dev) if need_db else None
-    a = MatmulBackwardArgs()
-    a.precision, a.M, a.N, a.K, a.act = _precision(x), M, N, K, act
-    a.dy, a.lddy = _matrix(dy, M, N, dt, "dy")
-    a.z, a.ldz = _matrix(z, M, N, dt, "z")
-    a.x, a.ldx = _matrix(x, M, K, dt, "x")
-    a.w, a.ldw = _matrix(w, N, K, dt, "w")
-    a.dz, a.lddz = _matrix(dz, M, N, dt, "dz")
-    a.dx, a.lddx = _matrix(dx, M, K, dt, "dx")
-    a.dw, a.db = _dev(dw), _dev(db)
-    a.dw_precision = EKYA_FP32 if dw_dtype == torch.float32 else EKYA_BF16
+        dx = torch.empty((M, K), dtype=dt, device=dev)
+    dw = torch.empty((N, K), dtype=dw_dtype, device=dev) if need_dw else None
+    db = torch.empty(N, dtype=f32, device=dev) if need_db else None
+    a = MatmulBackwardArgs(_precision(x), M, N, K, *_matrix(dy, M, N, dt, "dy"),
+                           *_matrix(z, M, N, dt, "z"), act, *_matrix(x, M, K, dt, "x"),
+                           *_matrix(w, N, K, dt, "w"), *_matrix(dz, M, N, dt, "dz"),
+                           *_matrix(dx, M, K, dt, "dx"), dw.data_ptr() if need_dw else None,
+                           EKYA_FP32 if dw_dtype == f32 else EKYA_BF16, db.data_ptr() if need_db else None)
     args = ctypes.byref(a)
     nbytes = lib.ekya_op_matmul_backward_workspace(args)
     ws = _scratch(nbytes, dev)
-    _op(lib.ekya_op_matmul_backward(args, _dev(ws), nbytes, _stream()))
+    _op(lib.ekya_op_matmul_backward(args, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(d)))
     return dx, dw, db, dz
 
 
@@ -914,13 +917,6 @@ class Adamw:
     __del__ = close
 
 
-def _adamw_grad(g, like, dtype):
-    if tuple(g.shape) != tuple(like.shape):
-        raise ValueError(f"gradient: expected shape {tuple(like.shape)}, got {tuple(g.shape)}")
-    _on_current(like, g)
-    return _dev(g, dtype)
-
-
 def ekya_adamw_create(tensors: Sequence[dict], state_bits: int = 32) -> Adamw:
     """tensors: dicts of w (fp32), g (fp32 or bf16), m and v (fp32; with 8 bits
     float8_e4m3fn and float8_e5m2), and as needed scale (8 bits: fp32
@@ -928,21 +924,19 @@ def ekya_adamw_create(tensors: Sequence[dict], state_bits: int = 32) -> Adamw:
     torch = _torch()
     if state_bits not in (8, 32):
         raise ValueError("state_bits must be 8 or 32")
-    kinds = (torch.float8_e4m3fn, torch.float8_e5m2) if state_bits == 8 else (torch.float32,) * 2
+    f32, bf16 = torch.float32, torch.bfloat16
+    mt, vt = (torch.float8_e4m3fn, torch.float8_e5m2) if state_bits == 8 else (f32, f32)
     arr = (AdamwTensor * max(1, len(tensors)))()
-    gtype = tensors[0]["g"].dtype if tensors else torch.float32
-    for a, t in zip(arr, tensors):
-        w, m, v, scale, low = t["w"], t["m"], t["v"], t.get("scale"), t.get("low")
-        _on_current(w, m, v, scale, low)
-        _shaped(m, w.shape, "m"), _shaped(v, w.shape, "v"), _shaped(low, w.shape, "low")
-        if scale is not None and scale.numel() != (w.numel() + 255) // 256 * 2:
-            raise ValueError("scale: expected two per 256 elements")
-        a.w, a.m, a.v = _dev(w, torch.float32), _dev(m, kinds[0]), _dev(v, kinds[1])
-        a.g = _adamw_grad(t["g"], w, gtype)
-        a.scale, a.low = _dev(scale, torch.float32), _dev(low, torch.bfloat16)
-        a.n, a.weight_decay = w.numel(), t.get("weight_decay", 0.0)
+    gtype = tensors[0]["g"].dtype if tensors else f32
+    for i, t in enumerate(tensors):
+        w, g, m, v, scale, low = t["w"], t["g"], t["m"], t["v"], t.get("scale"), t.get("low")
+        _on_current(w, g, m, v, scale, low)
+        shape, n = w.shape, w.numel()
+        arr[i] = AdamwTensor(_ptr(w, shape, f32, "w"), _ptr(g, shape, gtype, "g"), _ptr(m, shape, mt, "m"),
+                             _ptr(v, shape, vt, "v"), _ptr(scale, ((n + 255) // 256, 2), f32, "scale"),
+                             _ptr(low, shape, bf16, "low"), n, t.get("weight_decay", 0.0))
     h = ctypes.c_void_p()
-    prec = EKYA_FP32 if gtype == torch.float32 else EKYA_BF16 if gtype == torch.bfloat16 else -1
+    prec = EKYA_FP32 if gtype == f32 else EKYA_BF16 if gtype == bf16 else -1
     _op(load().ekya_adamw_create(ctypes.byref(h), arr, len(tensors), prec, state_bits))
     return Adamw(h, list(tensors), [t["g"] for t in tensors])
 
@@ -957,7 +951,8 @@ def ekya_adamw_set_grads(opt: Adamw, grads: Sequence) -> None:
         raise ValueError("one gradient per tensor")
     arr = (_P * max(1, len(grads)))()
     for i, (g, t) in enumerate(zip(grads, opt.tensors)):
-        arr[i] = _adamw_grad(g, t["w"], opt.grads[0].dtype)
+        _on_current(t["w"], g)
+        arr[i] = _ptr(g, t["w"].shape, opt.grads[0].dtype, "gradient")
     _op(load().ekya_adamw_set_grads(opt.handle, arr, len(grads)))
     opt.grads = list(grads)
 
@@ -967,16 +962,15 @@ def ekya_adamw_step(opt: Adamw, lr: float, beta1: float = 0.9, beta2: float = 0.
     """One step over every tensor.  step_device: an int64 tensor of one element on
     the GPU that holds the step's number when the kernels run."""
     torch = _torch()
-    if opt.device is not None and opt.device.index != torch.cuda.current_device():
+    d = torch.cuda.current_device()
+    if opt.device is not None and opt.device.index != d:
         raise ValueError("the optimizer's tensors live on another GPU")
     if step_device is not None:
-        if step_device.numel() != 1:
-            raise ValueError("step_device: expected one element")
-        if opt.device is not None and step_device.device != opt.device:
-            raise ValueError("tensors must live on one GPU")
-        step_device = _dev(step_device, torch.int64)
+        if step_device.get_device() != d:
+            raise ValueError("step_device must live on the current GPU")
+        step_device = _ptr(step_device.view(-1), (1,), torch.int64, "step_device")
     opts = AdamwOpts(lr, beta1, beta2, eps, step, step_device, seed)
-    _op(load().ekya_adamw_step(opt.handle, ctypes.byref(opts), _stream()))
+    _op(load().ekya_adamw_step(opt.handle, ctypes.byref(opts), _raw_stream(d)))
 
 
 # ---------------------------------------------------- scheduling layer (host)
