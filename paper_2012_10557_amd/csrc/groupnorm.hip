@@ -8,7 +8,9 @@
 // into groups by the coefficient kernels.  Means and squared deviations are
 // merged pairwise (Chan, Golub and LeVeque), so that a mean far from zero costs
 // no digits.
+#include <algorithm>
 #include <climits>
+#include <numeric>
 
 #include "act.hpp"
 #include "kernels.hpp"
@@ -37,6 +39,17 @@ template <typename T, int E> struct GnUnit {
     *reinterpret_cast<uint4*>(p) = t.u;
   }
 };
+template <> struct GnUnit<bf16, 4> {  // 8 bytes
+  uint2 u;
+  __device__ __forceinline__ void load(const bf16* p) { u = *reinterpret_cast<const uint2*>(p); }
+  __device__ __forceinline__ void get(float (&v)[4]) const {
+    v[0] = __uint_as_float(u.x << 16);
+    v[1] = __uint_as_float(u.x & 0xFFFF0000u);
+    v[2] = __uint_as_float(u.y << 16);
+    v[3] = __uint_as_float(u.y & 0xFFFF0000u);
+  }
+  static __device__ __forceinline__ void store(bf16* p, const float (&v)[4]) { store4(p, v); }
+};
 template <typename T> struct GnUnit<T, 1> {
   T u;
   __device__ __forceinline__ void load(const T* p) { u = *p; }
@@ -49,8 +62,8 @@ struct GnArgs {
   void* out;
   const float *gamma, *beta;  // null: 1 and 0
   float *mean, *rstd;         // [N][G]
-  float* part;                // [N][chunks][C][2]
-  float* tot;                 // [N][C][2] (backward)
+  float* part;                // [N][chunks][C][2] (backward: [2][C])
+  float* tot;                 // [N][2][C] (backward)
   float* coef;                // [N][G][2] (backward)
   float *dgamma, *dbeta;
   long long HW;
@@ -224,15 +237,25 @@ template <int E> struct GnChan {
       const int g = (c + e) / a.gs;
       mean[e] = a.mean[(long long)n * a.G + g];
       rstd[e] = a.rstd[(long long)n * a.G + g];
+    }
+    affine(a, c);
+  }
+  __device__ __forceinline__ void affine(const GnArgs& a, int c) {
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
       gamma[e] = a.gamma ? a.gamma[c + e] : 1.f;
       beta[e] = a.beta ? a.beta[c + e] : 0.f;
     }
   }
-  __device__ __forceinline__ float xhat(int e, float x) const { return (x - mean[e]) * rstd[e]; }
   // Rounded after every operation, so that forward and backward (and whoever
   // follows the formula in fp32) see the same sign at a ReLU.
+  __device__ __forceinline__ float xhat(int e, float x) const {
+#pragma clang fp contract(off)
+    return (x - mean[e]) * rstd[e];
+  }
   __device__ __forceinline__ float pre(int e, float xh) const {
-    return __fadd_rn(__fmul_rn(xh, gamma[e]), beta[e]);
+#pragma clang fp contract(off)
+    return xh * gamma[e] + beta[e];
   }
 };
 
@@ -256,7 +279,7 @@ __global__ __launch_bounds__(GN_NT) void gn_apply_kernel(GnArgs a) {
   }
 }
 
-// part[n][chunk][c] = (sum g, sum g * xhat) of the chunk's pixels.
+// part[n][chunk][2][c] = sum g, and sum g * xhat, of the chunk's pixels.
 template <typename T, int E, int ACT>
 __global__ __launch_bounds__(GN_NT) void gn_bwd_sums_kernel(GnArgs a) {
   __shared__ float red[GN_NT * E];
@@ -287,63 +310,70 @@ __global__ __launch_bounds__(GN_NT) void gn_bwd_sums_kernel(GnArgs a) {
   gn_row_sum<E>(s, red, a.cup);
   gn_row_sum<E>(q, red, a.cup);
   if (p.r == 0 && p.on) {
-    float* o = a.part + 2 * (((long long)p.n * a.chunks + p.chunk) * a.C + p.c);
+    float* o = a.part + 2 * ((long long)p.n * a.chunks + p.chunk) * a.C + p.c;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      o[2 * e] = s[e];
-      o[2 * e + 1] = q[e];
+      o[e] = s[e];
+      o[a.C + e] = q[e];
     }
   }
 }
 
-// tot[n][c] = sum of the sample's chunks.
-__global__ __launch_bounds__(GN_NT) void gn_bwd_fold_kernel(GnArgs a) {
-  const long long i = (long long)blockIdx.x * GN_NT + threadIdx.x, n = i / (2 * a.C);
-  if (n >= a.N) return;
-  const long long c = i - n * 2 * a.C;
-  const float* p = a.part + n * a.chunks * 2 * a.C + c;
+// tot[n][2][c] = sums over the sample's chunks of part[n][chunk][2][c]: 32
+// columns a block, 32 threads a column.
+__global__ __launch_bounds__(1024) void gn_bwd_fold_kernel(GnArgs a) {
+  __shared__ float red[32][33];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, per = (2 * a.C + 31) / 32;
+  const int n = blockIdx.x / per, c = (blockIdx.x - n * per) * 32 + x;
+  const float* p = a.part + (long long)n * a.chunks * 2 * a.C + c;
   float s = 0.f;
-  for (int k = 0; k < a.chunks; ++k) s += p[(long long)k * 2 * a.C];
-  a.tot[i] = s;
+  if (c < 2 * a.C)
+#pragma unroll 4
+    for (int k = y; k < a.chunks; k += 32) s += p[(long long)k * 2 * a.C];
+  red[y][x] = s;
+  __syncthreads();
+  for (int h = 16; h > 0; h >>= 1) {
+    if (y < h) red[y][x] += red[y + h][x];
+    __syncthreads();
+  }
+  if (y == 0 && c < 2 * a.C) a.tot[(long long)n * 2 * a.C + c] = red[0][x];
 }
 
-// Blocks below N * G: coef = (avg h, avg h * xhat) of a (sample, group); the
-// others: dgamma and dbeta of 64 channels, summed over the samples.
-__global__ __launch_bounds__(GN_NT) void gn_bwd_coef_kernel(GnArgs a, int groups) {
-  __shared__ float red[4][128];
-  const int t = threadIdx.x;
-  if ((int)blockIdx.x < groups) {
-    const int n = blockIdx.x / a.G, g = blockIdx.x - n * a.G;
-    const float* tot = a.tot + 2 * ((long long)n * a.C + g * a.gs);
-    float s = 0.f, q = 0.f;
-    for (int c = t; c < a.gs; c += GN_NT) {
-      const float w = a.gamma ? a.gamma[g * a.gs + c] : 1.f;
-      s += w * tot[2 * c];
-      q += w * tot[2 * c + 1];
-    }
-    s = block_sum(s, red[0]);
-    q = block_sum(q, red[0]);
-    const float inv = 1.f / ((float)a.HW * a.gs);
-    if (t == 0) {
-      a.coef[2 * (long long)blockIdx.x] = s * inv;
-      a.coef[2 * (long long)blockIdx.x + 1] = q * inv;
-    }
-    return;
-  }
-  const int c0 = ((int)blockIdx.x - groups) * 64, c = c0 + (t & 63);
+// coef = (avg h, avg h * xhat) of a (sample, group): a block each.
+__global__ __launch_bounds__(GN_NT) void gn_bwd_coef_kernel(GnArgs a) {
+  __shared__ float red[4];
+  const int t = threadIdx.x, n = blockIdx.x / a.G, g = blockIdx.x - n * a.G;
+  const float* tot = a.tot + (long long)n * 2 * a.C + g * a.gs;
   float s = 0.f, q = 0.f;
-  if (c < a.C)
-    for (int n = t >> 6; n < a.N; n += 4) {
-      const float* p = a.tot + 2 * ((long long)n * a.C + c);
-      s += p[0];
-      q += p[1];
-    }
-  red[t >> 6][t & 63] = s;
-  red[t >> 6][64 + (t & 63)] = q;
+  for (int c = t; c < a.gs; c += GN_NT) {
+    const float w = a.gamma ? a.gamma[g * a.gs + c] : 1.f;
+    s += w * tot[c];
+    q += w * tot[a.C + c];
+  }
+  s = block_sum(s, red);
+  q = block_sum(q, red);
+  const float inv = 1.f / ((float)a.HW * a.gs);
+  if (t == 0) {
+    a.coef[2 * (long long)blockIdx.x] = s * inv;
+    a.coef[2 * (long long)blockIdx.x + 1] = q * inv;
+  }
+}
+
+// dbeta and dgamma: tot summed over the samples.
+__global__ __launch_bounds__(1024) void gn_bwd_param_kernel(GnArgs a) {
+  __shared__ float red[32][33];
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+  float s = 0.f;
+  if (c < 2 * a.C)
+#pragma unroll 8
+    for (int n = y; n < a.N; n += 32) s += a.tot[(long long)n * 2 * a.C + c];
+  red[y][x] = s;
   __syncthreads();
-  if (t < 128 && c0 + (t & 63) < a.C)
-    (t < 64 ? a.dbeta : a.dgamma)[c0 + (t & 63)] =
-        (red[0][t] + red[1][t]) + (red[2][t] + red[3][t]);
+  for (int h = 16; h > 0; h >>= 1) {
+    if (y < h) red[y][x] += red[y + h][x];
+    __syncthreads();
+  }
+  if (y == 0 && c < 2 * a.C) (c < a.C ? a.dbeta + c : a.dgamma + (c - a.C))[0] = red[0][x];
 }
 
 template <typename T, int E, int ACT>
@@ -382,6 +412,235 @@ int next_pow2(int v) {
   int p = 1;
   while (p < v) p *= 2;
   return p;
+}
+
+// --------------------------------------------------------- one pass in all
+// A block takes whole groups of one sample, U units a row, and keeps them in
+// registers (up to R units a thread) from the sums to the results.  What runs
+// once is bound by fetching its instructions (a kernel of 6000 took 14 us for
+// one sample of 400 KB), so loops over registers end at the thread's units and
+// everything else is kept short.
+constexpr int GN_MOST = 1024;                          // threads of a block
+constexpr int GN_FWD_UNITS = 13;                       // most units of a thread, forward
+constexpr int GN_WIDE = 256;                           // most units of a row
+constexpr int GN_SLOTS = 16 * 64 * 4;                  // floats: 16 waves of 64 units of 4 channels
+
+struct GnFuse {
+  int U, up, lup, W;  // units of a row, the next power of two, its logarithm, channels
+  int rpp;            // rows of a pass
+  int lanes;          // that add up a group
+  int need;           // units of a thread
+  int chunks;         // blocks of a sample
+  int spread;         // samples go round the XCDs, so that blocks sharing cache lines share an L2
+};
+
+// A thread's place: its unit u of rows r, r + rpp, ..
+template <typename T, int E> struct GnSeat {
+  int n, c0, u, r;
+  bool on, last;       // whether it has a unit at all, and one in the last pass
+  uint32_t off, step;  // bytes from the sample's start, and from row to row
+  __device__ __forceinline__ bool init(const GnArgs& a, const GnFuse& f) {
+    const int b = blockIdx.x, k = f.spread ? b >> 3 : b;
+    n = k / f.chunks;
+    const int chunk = k - n * f.chunks;
+    if (f.spread) n = (b & 7) + 8 * n;
+    const int t = threadIdx.x;
+    u = t & (f.up - 1);
+    r = t >> f.lup;
+    c0 = chunk * f.W;
+    on = u < f.U;
+    last = on && r + (f.need - 1) * f.rpp < (int)a.HW;
+    off = ((uint32_t)r * a.C + c0 + u * E) * (uint32_t)sizeof(T);
+    step = (uint32_t)f.rpp * a.C * (uint32_t)sizeof(T);
+    return n < a.N;
+  }
+  // Pass i of f.need: whether this thread has a unit in it.
+  __device__ __forceinline__ bool has(const GnFuse& f, int i) const { return i + 1 < f.need ? on : last; }
+  __device__ __forceinline__ const T* at(const T* sample, int i) const {
+    return (const T*)((const char*)sample + (off + i * step));
+  }
+  __device__ __forceinline__ T* at(T* sample, int i) const { return (T*)((char*)sample + (off + i * step)); }
+};
+
+// red[slot][c] = sums of the block's channels over the lanes of a wave (over
+// one row, where a row is longer than a wave), all in a fixed order.
+template <int E>
+__device__ __forceinline__ void gn_lane_sums(const GnFuse& f, float (&v)[E], int u, bool on, float* red) {
+  const int t = threadIdx.x;
+  for (int o = f.up; o < 64; o <<= 1)
+#pragma unroll
+    for (int e = 0; e < E; ++e) v[e] += __shfl_xor(v[e], o, 64);
+  const int l = max(f.lup, 6);
+  if (on && (t & ((1 << l) - 1)) < f.up)
+#pragma unroll
+    for (int e = 0; e < E; ++e) red[(t >> l) * f.W + u * E + e] = v[e];
+}
+// gsum[g] = the sum of a group's channels over the slots, times gamma where
+// given: f.lanes lanes a group.
+__device__ __forceinline__ void gn_group_sums(const GnArgs& a, const GnFuse& f, const float* red,
+                                              const float* gamma, float* gsum) {
+  const int t = threadIdx.x, L = f.lanes, slots = blockDim.x >> max(f.lup, 6), groups = f.W / a.gs;
+  for (int g = t / L; g < groups; g += blockDim.x / L) {
+    float s = 0.f;
+    for (int c = g * a.gs + (t & (L - 1)); c < (g + 1) * a.gs; c += L) {
+      float k = 0.f;
+#pragma unroll 4
+      for (int i = 0; i < slots; ++i) k += red[i * f.W + c];
+      s += gamma ? k * gamma[c] : k;
+    }
+    for (int o = L / 2; o > 0; o >>= 1) s += __shfl_xor(s, o, 64);
+    gsum[g] = s;
+  }
+}
+// The sums of the groups of a unit's channels.
+template <int E>
+__device__ __forceinline__ void gn_spread(const GnArgs& a, const GnFuse& f, const float* gsum, int u, float (&out)[E]) {
+  int g = u < f.U ? u * E / a.gs : 0, rest = u < f.U ? u * E - g * a.gs : 0;
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    out[e] = gsum[g];
+    const bool next = ++rest == a.gs;
+    rest = next ? 0 : rest;
+    g = next && e + 1 < E ? g + 1 : g;
+  }
+}
+
+template <typename T, int E, int ACT, int R>
+__global__ __launch_bounds__(GN_MOST) void gn_fused_kernel(GnArgs a, GnFuse f) {
+  __shared__ float red[2][GN_SLOTS], gsum[2][GN_WIDE * E];
+  GnSeat<T, E> p;
+  if (!p.init(a, f)) return;
+  const T* x = (const T*)a.x + p.n * a.HW * a.C;
+  T* y = (T*)a.out + p.n * a.HW * a.C;
+  GnUnit<T, E> d[R];
+  float s[E] = {}, v[E];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (i < f.need && p.has(f, i)) d[i].load(p.at(x, i));
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (i < f.need && p.has(f, i)) {
+      d[i].get(v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) s[e] += v[e];
+    }
+  }
+  const float inv = 1.f / ((float)a.HW * a.gs);
+  GnChan<E> ch;
+  gn_lane_sums(f, s, p.u, p.on, red[0]);
+  __syncthreads();
+  gn_group_sums(a, f, red[0], nullptr, gsum[0]);
+  __syncthreads();
+  gn_spread(a, f, gsum[0], p.u, ch.mean);
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    ch.mean[e] *= inv;
+    s[e] = 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (i < f.need && p.has(f, i)) {
+      d[i].get(v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        v[e] -= ch.mean[e];
+        s[e] += v[e] * v[e];
+      }
+    }
+  }
+  gn_lane_sums(f, s, p.u, p.on, red[1]);
+  __syncthreads();
+  gn_group_sums(a, f, red[1], nullptr, gsum[1]);
+  __syncthreads();
+  const long long g0 = (long long)p.n * a.G + p.c0 / a.gs;
+  for (int g = threadIdx.x; g < f.W / a.gs; g += blockDim.x) {
+    a.mean[g0 + g] = gsum[0][g] * inv;
+    a.rstd[g0 + g] = 1.f / sqrtf(gsum[1][g] * inv + a.eps);
+  }
+  if (!p.on) return;
+  gn_spread(a, f, gsum[1], p.u, ch.rstd);
+#pragma unroll
+  for (int e = 0; e < E; ++e) ch.rstd[e] = 1.f / sqrtf(ch.rstd[e] * inv + a.eps);
+  ch.affine(a, p.c0 + p.u * E);
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (i < f.need && p.has(f, i)) {
+      d[i].get(v);
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] = act_fwd<ACT, T>(ch.pre(e, ch.xhat(e, v[e])));
+      GnUnit<T, E>::store(p.at(y, i), v);
+    }
+  }
+}
+
+template <typename T, int E, int ACT, int R>
+__global__ __launch_bounds__(GN_MOST) void gn_fused_bwd_kernel(GnArgs a, GnFuse f) {
+  __shared__ float red[2][GN_SLOTS], gsum[2][GN_WIDE * E];
+  GnSeat<T, E> p;
+  if (!p.init(a, f)) return;
+  const T* x = (const T*)a.x + p.n * a.HW * a.C;
+  const T* dy = (const T*)a.dy + p.n * a.HW * a.C;
+  T* dx = (T*)a.out + p.n * a.HW * a.C;
+  GnUnit<T, E> ux[R], uy[R];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (i < f.need && p.has(f, i)) {
+      ux[i].load(p.at(x, i));
+      uy[i].load(p.at(dy, i));
+    }
+  }
+  GnChan<E> ch;
+  if (p.on) ch.load(a, p.n, p.c0 + p.u * E);
+  float s[E] = {}, q[E] = {}, v[E], w[E];
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (i < f.need && p.has(f, i)) {
+      ux[i].get(v);
+      uy[i].get(w);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float xh = ch.xhat(e, v[e]), g = act_bwd<ACT, T>(w[e], ch.pre(e, xh));
+        s[e] += g;
+        q[e] += g * xh;
+      }
+    }
+  }
+  const float inv = 1.f / ((float)a.HW * a.gs), *gamma = a.gamma ? a.gamma + p.c0 : nullptr;
+  gn_lane_sums(f, s, p.u, p.on, red[0]);
+  gn_lane_sums(f, q, p.u, p.on, red[1]);
+  __syncthreads();
+  gn_group_sums(a, f, red[0], gamma, gsum[0]);
+  gn_group_sums(a, f, red[1], gamma, gsum[1]);
+  for (int c = threadIdx.x; c < 2 * f.W; c += blockDim.x) {  // the channels' totals
+    const int w = c >= f.W, k = c - w * f.W, slots = blockDim.x >> max(f.lup, 6);
+    float sum = 0.f;
+#pragma unroll 4
+    for (int i = 0; i < slots; ++i) sum += red[w][i * f.W + k];
+    a.tot[((long long)p.n * 2 + w) * a.C + p.c0 + k] = sum;
+  }
+  __syncthreads();
+  if (!p.on) return;
+  gn_spread(a, f, gsum[0], p.u, s);
+  gn_spread(a, f, gsum[1], p.u, q);
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    s[e] *= inv;
+    q[e] *= inv;
+  }
+#pragma unroll
+  for (int i = 0; i < R; ++i) {
+    if (i < f.need && p.has(f, i)) {
+      ux[i].get(v);
+      uy[i].get(w);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        const float xh = ch.xhat(e, v[e]), h = act_bwd<ACT, T>(w[e], ch.pre(e, xh)) * ch.gamma[e];
+        v[e] = ch.rstd[e] * (h - s[e] - xh * q[e]);
+      }
+      GnUnit<T, E>::store(p.at(dx, i), v);
+    }
+  }
 }
 
 // How a call is cut.  Chunks of pixels: 8 per thread at least, and no more
@@ -424,7 +683,60 @@ template <typename F> hipError_t gn_samples(GnArgs a, size_t esize, long long pe
   return hipSuccess;
 }
 
+// Threads and channels of the one-pass kernels, or false where a block cannot
+// hold its groups: `most` units a thread.  Rows of a block are 128 bytes wide
+// where that leaves 512 blocks.
+bool gn_fuse(const GnArgs& a, int E, int bytes, int most, GnFuse& f, int& threads) {
+  if (a.HW > GN_MOST * most || a.N > (1 << 20)) return false;
+  const int base = a.gs / std::gcd(a.gs, E) * E, pieces = a.C / base;  // whole groups, whole units
+  if (a.C % base) return false;
+  auto fits = [&](int k) {
+    const int up = next_pow2(base * k / E);
+    return up <= GN_WIDE && a.HW <= (long long)GN_MOST / up * most;
+  };
+  int k = 1;
+  for (int j = 2; j <= pieces && base * k * bytes < 128; ++j)
+    if (pieces % j == 0 && fits(j) && (long long)a.N * (pieces / j) >= 512) k = j;
+  if (!fits(k) || (k < pieces && base * k * bytes < 32 && (long long)a.N * a.HW * a.C > (1 << 20))) return false;
+  f.W = base * k;
+  f.U = f.W / E;
+  f.up = next_pow2(f.U);
+  f.chunks = a.C / f.W;
+  f.spread = a.N >= 64 && f.chunks > 1;
+  threads = 64;
+  while (threads < GN_MOST && (threads * 2 < a.HW * f.up || threads < f.up)) threads *= 2;
+  f.rpp = threads / f.up;
+  f.need = (int)cdivl(a.HW, f.rpp);
+  f.lup = 0;
+  while (1 << f.lup < f.up) ++f.lup;
+  f.lanes = 64;
+  while (f.lanes > 1 && (f.lanes * (f.W / a.gs) > threads || f.lanes / 2 >= a.gs)) f.lanes /= 2;
+  return f.need <= most;
+}
+
+template <typename T, int E, typename F>
+hipError_t gn_fused_samples(const GnArgs& a, const GnFuse& f, F&& go) {
+  return gn_samples(a, sizeof(T), f.chunks, [&](const GnArgs& b, dim3) {
+    return go(b, dim3((unsigned)((f.spread ? (b.N + 7) / 8 * 8 : b.N) * f.chunks)));
+  });
+}
+
 template <typename T, int E> hipError_t gn_forward(GnArgs a, int act, hipStream_t st) {
+  if constexpr (E > 1) {
+    constexpr int EU = 4;
+    GnFuse f;
+    int threads;
+    if (gn_fuse(a, EU, sizeof(T), GN_FWD_UNITS, f, threads))
+      return gn_fused_samples<T, EU>(a, f, [&](const GnArgs& b, dim3 grid) {
+        return act_dispatch(act, [&](auto k) {
+          if (f.need <= 3)
+            hipLaunchKernelGGL((gn_fused_kernel<T, EU, k.value, 3>), grid, dim3(threads), 0, st, b, f);
+          else
+            hipLaunchKernelGGL((gn_fused_kernel<T, EU, k.value, GN_FWD_UNITS>), grid, dim3(threads), 0, st, b, f);
+          return hipGetLastError();
+        });
+      });
+  }
   gn_cut(a, E);
   const long long per = (long long)a.chunks * a.cchunks;
   EKYA_HIP(gn_samples(a, sizeof(T), per, [&](const GnArgs& b, dim3 grid) {
@@ -444,6 +756,28 @@ template <typename T, int E> hipError_t gn_forward(GnArgs a, int act, hipStream_
 }
 
 template <typename T, int E> hipError_t gn_backward(GnArgs a, int act, hipStream_t st) {
+  if constexpr (E > 1) {
+    // 8-byte units in bf16: a unit's constants and sums take half the registers
+    constexpr int EU = 4, R = sizeof(T) == 2 ? 13 : 7;
+    GnFuse f;
+    int threads;
+    if (gn_fuse(a, EU, sizeof(T), R, f, threads)) {
+      EKYA_HIP((gn_fused_samples<T, EU>(a, f, [&](const GnArgs& b, dim3 grid) {
+        return act_dispatch(act, [&](auto k) {
+          if (f.need <= 3)
+            hipLaunchKernelGGL((gn_fused_bwd_kernel<T, EU, k.value, 3>), grid, dim3(threads), 0, st, b, f);
+          else
+            hipLaunchKernelGGL((gn_fused_bwd_kernel<T, EU, k.value, R>), grid, dim3(threads), 0, st, b, f);
+          return hipGetLastError();
+        });
+      })));
+      if (a.dgamma) {
+        hipLaunchKernelGGL(gn_bwd_param_kernel, dim3(cdiv(2 * a.C, 32)), dim3(1024), 0, st, a);
+        EKYA_HIP(hipGetLastError());
+      }
+      return hipSuccess;
+    }
+  }
   gn_cut(a, E);
   const long long per = (long long)a.chunks * a.cchunks;
   EKYA_HIP(gn_samples(a, sizeof(T), per, [&](const GnArgs& b, dim3 grid) {
@@ -452,18 +786,16 @@ template <typename T, int E> hipError_t gn_backward(GnArgs a, int act, hipStream
       return hipGetLastError();
     });
   }));
-  EKYA_HIP(gn_samples(a, sizeof(T), cdiv(2 * a.C, GN_NT), [&](const GnArgs& b, dim3) {
-    hipLaunchKernelGGL(gn_bwd_fold_kernel, dim3((unsigned)cdivl((long long)b.N * 2 * a.C, GN_NT)),
-                       dim3(GN_NT), 0, st, b);
+  EKYA_HIP(gn_samples(a, sizeof(T), cdiv(2 * a.C, 32), [&](const GnArgs& b, dim3 grid) {
+    hipLaunchKernelGGL(gn_bwd_fold_kernel, grid, dim3(1024), 0, st, b);
     return hipGetLastError();
   }));
-  const int dparam = a.dgamma ? cdiv(a.C, 64) : 0;
   EKYA_HIP(gn_samples(a, sizeof(T), a.G, [&](const GnArgs& b, dim3 grid) {
-    hipLaunchKernelGGL(gn_bwd_coef_kernel, grid, dim3(GN_NT), 0, st, b, (int)grid.x);
+    hipLaunchKernelGGL(gn_bwd_coef_kernel, grid, dim3(GN_NT), 0, st, b);
     return hipGetLastError();
   }));
-  if (dparam) {
-    hipLaunchKernelGGL(gn_bwd_coef_kernel, dim3(dparam), dim3(GN_NT), 0, st, a, 0);
+  if (a.dgamma) {
+    hipLaunchKernelGGL(gn_bwd_param_kernel, dim3(cdiv(2 * a.C, 32)), dim3(1024), 0, st, a);
     EKYA_HIP(hipGetLastError());
   }
   return gn_samples(a, sizeof(T), per, [&](const GnArgs& b, dim3 grid) {
