@@ -39,6 +39,14 @@ template <typename T, int E> struct GnUnit {
     *reinterpret_cast<uint4*>(p) = t.u;
   }
 };
+// Between two passes over units in registers: the compiler would keep the first
+// pass's unpacked values for the second, in twice the registers.
+__device__ __forceinline__ void gn_renew(uint4& u) {
+  asm volatile("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w));
+}
+__device__ __forceinline__ void gn_renew(uint2& u) { asm volatile("" : "+v"(u.x), "+v"(u.y)); }
+template <typename U> __device__ __forceinline__ void gn_renew(U&) {}
+
 template <> struct GnUnit<bf16, 4> {  // 8 bytes
   uint2 u;
   __device__ __forceinline__ void load(const bf16* p) { u = *reinterpret_cast<const uint2*>(p); }
@@ -62,7 +70,7 @@ struct GnArgs {
   void* out;
   const float *gamma, *beta;  // null: 1 and 0
   float *mean, *rstd;         // [N][G]
-  float* part;                // [N][chunks][C][2] (backward: [2][C])
+  float* part;                // [N][slots][C][2] (backward: [N][chunks][2][C])
   float* tot;                 // [N][2][C] (backward)
   float* coef;                // [N][G][2] (backward)
   float *dgamma, *dbeta;
@@ -70,6 +78,7 @@ struct GnArgs {
   int N, C, G, gs;       // gs: channels of a group
   int cu, cup, cchunks;  // units of a channel chunk, the next power of two, chunks
   int rows, chunks;      // pixels of a chunk, chunks of a sample
+  int srows, slots;      // the same for a wave of the statistics pass
   float eps;
 };
 
@@ -96,15 +105,6 @@ template <int E> __device__ __forceinline__ GnPlace gn_place(const GnArgs& a) {
   return p;
 }
 
-// (n, mean, m2) += (nb, meanb, m2b): counts as floats, nb > 0.
-__device__ __forceinline__ void chan_merge(float& n, float& mean, float& m2, float nb, float meanb,
-                                           float m2b) {
-  const float t = n + nb, d = meanb - mean, f = t > 0.f ? nb / t : 0.f;
-  mean += d * f;
-  m2 += m2b + d * d * (n * f);
-  n = t;
-}
-
 // Sums v over the threads of a block that share a channel unit, in a fixed
 // order; threads of the first row return the totals.  red: GN_NT * E floats.
 template <int E> __device__ __forceinline__ void gn_row_sum(float (&v)[E], float* red, int cup) {
@@ -122,30 +122,36 @@ template <int E> __device__ __forceinline__ void gn_row_sum(float (&v)[E], float
   for (int e = 0; e < E; ++e) v[e] = red[threadIdx.x * E + e];
 }
 
-// part[n][chunk][c] = (mean, squared deviations) of the chunk's pixels.
+// part[n][slot][c] = (mean, squared deviations) of a slot's pixels: a wave
+// each, whose lanes keep a unit and walk its rows.  Lanes merge by shuffles,
+// without a barrier (with sums over the block through LDS 128 x 3136 x 64 took 24
+// us for this pass).
 template <typename T, int E> __global__ __launch_bounds__(GN_NT) void gn_stats_kernel(GnArgs a) {
-  __shared__ float red[GN_NT * E];
-  const GnPlace p = gn_place<E>(a);
-  const T* x = (const T*)a.x + p.n * a.HW * a.C + p.c;
+  constexpr int S = E == 8 ? 4 : GN_R;  // units of a lane at once
+  const int lane = threadIdx.x & 63, groups = cdiv(a.slots, GN_NT / 64), per = groups * a.cchunks;
+  const int n = blockIdx.x / per, rest = blockIdx.x - n * per, cc = rest % a.cchunks;
+  const int slot = rest / a.cchunks * (GN_NT / 64) + (threadIdx.x >> 6);
+  if (slot >= a.slots) return;
+  const int u = lane & (a.cup - 1), rpp = 64 / a.cup, c = (cc * a.cu + u) * E;
+  const long long r0 = (long long)slot * a.srows + lane / a.cup, r1 = min(a.HW, (slot + 1LL) * a.srows);
+  const bool on = u < a.cu && c < a.C;
+  const T* x = (const T*)a.x + n * a.HW * a.C + c;
   float cnt = 0.f, mean[E], m2[E];
 #pragma unroll
   for (int e = 0; e < E; ++e) mean[e] = m2[e] = 0.f;
-  for (long long r = p.r0 + p.r; p.on && r < p.r1; r += (long long)GN_R * p.rpp) {
-    GnUnit<T, E> u[GN_R];
-    int k = 0;
-#pragma unroll
-    for (int i = 0; i < GN_R; ++i)
-      if (r + (long long)i * p.rpp < p.r1) {
-        u[i].load(x + (r + (long long)i * p.rpp) * a.C);
-        ++k;
-      }
+  for (long long r = r0; on && r < r1; r += (long long)S * rpp) {
+    GnUnit<T, E> d[S];
+    const int k = (int)min((long long)S, (r1 - r + rpp - 1) / rpp);
     float s[E], q[E], v[E];
+#pragma unroll
+    for (int i = 0; i < S; ++i)
+      if (i < k) d[i].load(x + (r + (long long)i * rpp) * a.C);
 #pragma unroll
     for (int e = 0; e < E; ++e) s[e] = q[e] = 0.f;
 #pragma unroll
-    for (int i = 0; i < GN_R; ++i)
+    for (int i = 0; i < S; ++i)
       if (i < k) {
-        u[i].get(v);
+        d[i].get(v);
 #pragma unroll
         for (int e = 0; e < E; ++e) s[e] += v[e];
       }
@@ -153,41 +159,43 @@ template <typename T, int E> __global__ __launch_bounds__(GN_NT) void gn_stats_k
 #pragma unroll
     for (int e = 0; e < E; ++e) s[e] *= inv;
 #pragma unroll
-    for (int i = 0; i < GN_R; ++i)
+    for (int i = 0; i < S; ++i)
       if (i < k) {
-        u[i].get(v);
+        gn_renew(d[i].u);
+        d[i].get(v);
 #pragma unroll
         for (int e = 0; e < E; ++e) q[e] += (v[e] - s[e]) * (v[e] - s[e]);
       }
-    const float n0 = cnt;
+    const float t = cnt + k, f = k / t, w = cnt * f;
+    cnt = t;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      cnt = n0;
-      chan_merge(cnt, mean[e], m2[e], (float)k, s[e], q[e]);
+      const float d = s[e] - mean[e];
+      mean[e] += d * f;
+      m2[e] += q[e] + d * d * w;
     }
   }
-  // the chunk's mean, then the deviations from it
-  const float total = (float)(p.r1 - p.r0);
-  float s[E], d[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) s[e] = mean[e] * (cnt / total);
-  gn_row_sum<E>(s, red, a.cup);
-  if (p.r == 0)
-#pragma unroll
-    for (int e = 0; e < E; ++e) red[threadIdx.x * E + e] = s[e];
-  __syncthreads();
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    s[e] = red[(threadIdx.x & (a.cup - 1)) * E + e];
-    d[e] = m2[e] + cnt * (mean[e] - s[e]) * (mean[e] - s[e]);
-  }
-  gn_row_sum<E>(d, red, a.cup);
-  if (p.r == 0 && p.on) {
-    float* o = a.part + 2 * (((long long)p.n * a.chunks + p.chunk) * a.C + p.c);
+  for (int o = a.cup; o < 64; o <<= 1) {
+    // both lanes of a pair get the same bits: the lower one's values come first
+    const float other = __shfl_xor(cnt, o, 64);
+    const bool upper = lane & o;
+    const float n0 = upper ? other : cnt, n1 = upper ? cnt : other, t = n0 + n1;
+    const float f = t > 0.f ? n1 / t : 0.f, w = n0 * f;
+    cnt = t;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
-      o[2 * e] = s[e];
-      o[2 * e + 1] = d[e];
+      const float om = __shfl_xor(mean[e], o, 64), oq = __shfl_xor(m2[e], o, 64);
+      const float ma = upper ? om : mean[e], d = (upper ? mean[e] : om) - ma;
+      mean[e] = ma + d * f;
+      m2[e] += oq + d * d * w;
+    }
+  }
+  if (on && lane < a.cup) {
+    float* o = a.part + 2 * (((long long)n * a.slots + slot) * a.C + c);
+#pragma unroll
+    for (int e = 0; e < E; ++e) {
+      o[2 * e] = mean[e];
+      o[2 * e + 1] = m2[e];
     }
   }
 }
@@ -201,25 +209,25 @@ __device__ __forceinline__ float block_sum(float v, float* red) {  // red: 4 flo
   return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
-// mean and rstd of a (sample, group) from its chunks' channels: a block each.
+// mean and rstd of a (sample, group) from its slots' channels: a block each.
 __global__ __launch_bounds__(GN_NT) void gn_mean_kernel(GnArgs a) {
   __shared__ float red[4];
   const int n = blockIdx.x / a.G, g = blockIdx.x - n * a.G;
-  const float* part = a.part + 2 * ((long long)n * a.chunks * a.C + g * a.gs);
-  const int count = a.chunks * a.gs;
+  const float* part = a.part + 2 * ((long long)n * a.slots * a.C + g * a.gs);
+  const int count = a.slots * a.gs;
   const float inv = 1.f / ((float)a.HW * a.gs);
-  const float last = (float)(a.HW - (long long)(a.chunks - 1) * a.rows);
+  const float last = (float)(a.HW - (a.slots - 1LL) * a.srows);
   float s = 0.f;
   for (int i = threadIdx.x; i < count; i += GN_NT) {
     const int k = i / a.gs, c = i - k * a.gs;
-    s += part[2 * ((long long)k * a.C + c)] * ((k == a.chunks - 1 ? last : (float)a.rows) * inv);
+    s += part[2 * ((long long)k * a.C + c)] * ((k == a.slots - 1 ? last : (float)a.srows) * inv);
   }
   const float mean = block_sum(s, red);
   float q = 0.f;
   for (int i = threadIdx.x; i < count; i += GN_NT) {
     const int k = i / a.gs, c = i - k * a.gs;
     const float* p = part + 2 * ((long long)k * a.C + c);
-    q += p[1] + (k == a.chunks - 1 ? last : (float)a.rows) * (p[0] - mean) * (p[0] - mean);
+    q += p[1] + (k == a.slots - 1 ? last : (float)a.srows) * (p[0] - mean) * (p[0] - mean);
   }
   const float var = block_sum(q, red) * inv;
   if (threadIdx.x == 0) {
@@ -268,14 +276,21 @@ __global__ __launch_bounds__(GN_NT) void gn_apply_kernel(GnArgs a) {
   const long long base = p.n * a.HW * a.C + p.c;
   const T* x = (const T*)a.x + base;
   T* y = (T*)a.out + base;
-  for (long long r = p.r0 + p.r; r < p.r1; r += p.rpp) {
-    GnUnit<T, E> u;
-    float v[E];
-    u.load(x + r * a.C);
-    u.get(v);
+  constexpr int A = 4;  // loads in flight
+  for (long long r = p.r0 + p.r; r < p.r1; r += (long long)A * p.rpp) {
+    GnUnit<T, E> u[A];
 #pragma unroll
-    for (int e = 0; e < E; ++e) v[e] = act_fwd<ACT, T>(ch.pre(e, ch.xhat(e, v[e])));
-    GnUnit<T, E>::store(y + r * a.C, v);
+    for (int i = 0; i < A; ++i)
+      if (r + i * p.rpp < p.r1) u[i].load(x + (r + i * p.rpp) * a.C);
+#pragma unroll
+    for (int i = 0; i < A; ++i)
+      if (r + i * p.rpp < p.r1) {
+        float v[E];
+        u[i].get(v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) v[e] = act_fwd<ACT, T>(ch.pre(e, ch.xhat(e, v[e])));
+        GnUnit<T, E>::store(y + (r + i * p.rpp) * a.C, v);
+      }
   }
 }
 
@@ -421,9 +436,8 @@ int next_pow2(int v) {
 // one sample of 400 KB), so loops over registers end at the thread's units and
 // everything else is kept short.
 constexpr int GN_MOST = 1024;                          // threads of a block
-constexpr int GN_FWD_UNITS = 13;                       // most units of a thread, forward
 constexpr int GN_WIDE = 256;                           // most units of a row
-constexpr int GN_SLOTS = 16 * 64 * 4;                  // floats: 16 waves of 64 units of 4 channels
+template <int E> constexpr int GN_SLOTS = 16 * 64 * E;  // floats: 16 waves of 64 units
 
 struct GnFuse {
   int U, up, lup, W;  // units of a row, the next power of two, its logarithm, channels
@@ -507,7 +521,7 @@ __device__ __forceinline__ void gn_spread(const GnArgs& a, const GnFuse& f, cons
 
 template <typename T, int E, int ACT, int R>
 __global__ __launch_bounds__(GN_MOST) void gn_fused_kernel(GnArgs a, GnFuse f) {
-  __shared__ float red[2][GN_SLOTS], gsum[2][GN_WIDE * E];
+  __shared__ float red[2][GN_SLOTS<E>], gsum[2][GN_WIDE * E];
   GnSeat<T, E> p;
   if (!p.init(a, f)) return;
   const T* x = (const T*)a.x + p.n * a.HW * a.C;
@@ -541,6 +555,7 @@ __global__ __launch_bounds__(GN_MOST) void gn_fused_kernel(GnArgs a, GnFuse f) {
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     if (i < f.need && p.has(f, i)) {
+      gn_renew(d[i].u);
       d[i].get(v);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
@@ -566,6 +581,7 @@ __global__ __launch_bounds__(GN_MOST) void gn_fused_kernel(GnArgs a, GnFuse f) {
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     if (i < f.need && p.has(f, i)) {
+      gn_renew(d[i].u);
       d[i].get(v);
 #pragma unroll
       for (int e = 0; e < E; ++e) v[e] = act_fwd<ACT, T>(ch.pre(e, ch.xhat(e, v[e])));
@@ -576,7 +592,7 @@ __global__ __launch_bounds__(GN_MOST) void gn_fused_kernel(GnArgs a, GnFuse f) {
 
 template <typename T, int E, int ACT, int R>
 __global__ __launch_bounds__(GN_MOST) void gn_fused_bwd_kernel(GnArgs a, GnFuse f) {
-  __shared__ float red[2][GN_SLOTS], gsum[2][GN_WIDE * E];
+  __shared__ float red[2][GN_SLOTS<E>], gsum[2][GN_WIDE * E];
   GnSeat<T, E> p;
   if (!p.init(a, f)) return;
   const T* x = (const T*)a.x + p.n * a.HW * a.C;
@@ -631,6 +647,8 @@ __global__ __launch_bounds__(GN_MOST) void gn_fused_bwd_kernel(GnArgs a, GnFuse 
 #pragma unroll
   for (int i = 0; i < R; ++i) {
     if (i < f.need && p.has(f, i)) {
+      gn_renew(ux[i].u);
+      gn_renew(uy[i].u);
       ux[i].get(v);
       uy[i].get(w);
 #pragma unroll
@@ -658,6 +676,12 @@ void gn_cut(GnArgs& a, int E) {
   rows = cdivl(rows, least) * least;
   a.rows = (int)std::min<long long>(rows, INT_MAX);
   a.chunks = (int)cdivl(a.HW, a.rows);
+  // slots: 16 units a lane, no more than 512 a sample (a block reads those of a
+  // group), nor than give 8192 waves
+  const long long few = (long long)GN_R * 2 * (64 / a.cup);
+  const long long most = std::min<long long>(512, std::max<long long>(4, 8192 / std::max(1LL, blocks)));
+  a.srows = (int)std::min<long long>(cdivl(std::max(few, cdivl(a.HW, most)), few) * few, INT_MAX);
+  a.slots = (int)cdivl(a.HW, a.srows);
 }
 
 bool unit_ok(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
@@ -675,7 +699,7 @@ template <typename F> hipError_t gn_samples(GnArgs a, size_t esize, long long pe
     b.out = (char*)a.out + off;
     b.mean = a.mean + n * a.G;
     b.rstd = a.rstd + n * a.G;
-    b.part = a.part + n * a.chunks * 2 * a.C;
+    b.part = a.part + n * std::max(a.chunks, a.slots) * 2 * a.C;
     if (a.tot) b.tot = a.tot + n * 2 * a.C;
     if (a.coef) b.coef = a.coef + n * 2 * a.G;
     EKYA_HIP(go(b, dim3((unsigned)(b.N * per))));
@@ -723,23 +747,23 @@ hipError_t gn_fused_samples(const GnArgs& a, const GnFuse& f, F&& go) {
 
 template <typename T, int E> hipError_t gn_forward(GnArgs a, int act, hipStream_t st) {
   if constexpr (E > 1) {
-    constexpr int EU = 4;
+    constexpr int EU = 4, R = 13;
     GnFuse f;
     int threads;
-    if (gn_fuse(a, EU, sizeof(T), GN_FWD_UNITS, f, threads))
+    if (gn_fuse(a, EU, sizeof(T), R, f, threads))
       return gn_fused_samples<T, EU>(a, f, [&](const GnArgs& b, dim3 grid) {
         return act_dispatch(act, [&](auto k) {
           if (f.need <= 3)
             hipLaunchKernelGGL((gn_fused_kernel<T, EU, k.value, 3>), grid, dim3(threads), 0, st, b, f);
           else
-            hipLaunchKernelGGL((gn_fused_kernel<T, EU, k.value, GN_FWD_UNITS>), grid, dim3(threads), 0, st, b, f);
+            hipLaunchKernelGGL((gn_fused_kernel<T, EU, k.value, R>), grid, dim3(threads), 0, st, b, f);
           return hipGetLastError();
         });
       });
   }
   gn_cut(a, E);
   const long long per = (long long)a.chunks * a.cchunks;
-  EKYA_HIP(gn_samples(a, sizeof(T), per, [&](const GnArgs& b, dim3 grid) {
+  EKYA_HIP(gn_samples(a, sizeof(T), cdivl(a.slots, GN_NT / 64) * a.cchunks, [&](const GnArgs& b, dim3 grid) {
     hipLaunchKernelGGL((gn_stats_kernel<T, E>), grid, dim3(GN_NT), 0, st, b);
     return hipGetLastError();
   }));
@@ -818,7 +842,7 @@ GnArgs gn_args(int N, long long HW, int C, int G) {
 
 size_t gn_part_floats(GnArgs a, int E) {
   gn_cut(a, E);
-  return (size_t)a.N * a.chunks * 2 * a.C;
+  return (size_t)a.N * std::max(a.chunks, a.slots) * 2 * a.C;
 }
 
 }  // namespace
