@@ -806,13 +806,23 @@ bool matmul_sizes_ok(int precision, long long M, int N, int K) {
          K <= (1 << 24) && M <= (1LL << 40) / std::max(N, K);
 }
 
+ekya::MatmulFwd matmul_call(const ekya_matmul_args& a) {
+  return {a.precision, a.M,   a.N,        a.K,   a.x,              a.ldx,
+          a.w,         a.ldw, a.bias,     a.act, a.residual,       a.ldr,
+          a.residual_first,   a.y,        a.ldy, a.z,              a.ldz};
+}
+ekya::MatmulBwd matmul_call(const ekya_matmul_backward_args& a) {
+  return {a.precision, a.M,    a.N,  a.K,    a.dy, a.lddy, a.z,  a.ldz,          a.act, a.x,
+          a.ldx,       a.w,    a.ldw, a.dz,  a.lddz, a.dx, a.lddx, a.dw, a.dw_precision, a.db};
+}
+
 }  // namespace
 
 extern "C" {
 
 size_t ekya_op_matmul_workspace(const ekya_matmul_args* a) {
   if (!a || !matmul_sizes_ok(a->precision, a->M, a->N, a->K)) return 0;
-  return ekya::matmul_workspace_floats(a->precision, a->M, a->N, a->K) * sizeof(float);
+  return ekya::matmul_workspace_floats(matmul_call(*a)) * sizeof(float);
 }
 
 ekya_status ekya_op_matmul(const ekya_matmul_args* args, void* workspace, size_t workspace_bytes,
@@ -836,16 +846,12 @@ ekya_status ekya_op_matmul(const ekya_matmul_args* args, void* workspace, size_t
     return fail(nullptr, EKYA_ERR_INVALID_ARG, "matmul: an output overlaps another matrix");
   const size_t need = ekya_op_matmul_workspace(args);
   if (ekya_status s = check_workspace("matmul", workspace, workspace_bytes, need)) return s;
-  const ekya::MatmulFwd f{a.precision, a.M,   a.N,        a.K,   a.x,              a.ldx,
-                          a.w,         a.ldw, a.bias,     a.act, a.residual,       a.ldr,
-                          a.residual_first,   a.y,        a.ldy, a.z,              a.ldz};
-  return hip_status(ekya::matmul_fwd(f, (float*)workspace, (hipStream_t)stream));
+  return hip_status(ekya::matmul_fwd(matmul_call(a), (float*)workspace, (hipStream_t)stream));
 }
 
 size_t ekya_op_matmul_backward_workspace(const ekya_matmul_backward_args* a) {
   if (!a || !matmul_sizes_ok(a->precision, a->M, a->N, a->K)) return 0;
-  return ekya::matmul_backward_workspace_floats(a->precision, a->M, a->N, a->K, a->dx, a->dw, a->db) *
-         sizeof(float);
+  return ekya::matmul_backward_workspace_floats(matmul_call(*a)) * sizeof(float);
 }
 
 ekya_status ekya_op_matmul_backward(const ekya_matmul_backward_args* args, void* workspace,
@@ -878,9 +884,7 @@ ekya_status ekya_op_matmul_backward(const ekya_matmul_backward_args* args, void*
   }
   const size_t need = ekya_op_matmul_backward_workspace(args);
   if (ekya_status s = check_workspace("matmul_backward", workspace, workspace_bytes, need)) return s;
-  const ekya::MatmulBwd f{a.precision, a.M,    a.N,  a.K,    a.dy, a.lddy, a.z,  a.ldz,          a.act, a.x,
-                          a.ldx,       a.w,    a.ldw, a.dz,  a.lddz, a.dx, a.lddx, a.dw, a.dw_precision, a.db};
-  return hip_status(ekya::matmul_bwd(f, (float*)workspace, (hipStream_t)stream));
+  return hip_status(ekya::matmul_bwd(matmul_call(a), (float*)workspace, (hipStream_t)stream));
 }
 
 }  // extern "C"

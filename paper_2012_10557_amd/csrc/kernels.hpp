@@ -435,9 +435,9 @@ struct MatmulBwd {
   int dw_dt;
   float* db;
 };
-size_t matmul_workspace_floats(int dt, long long M, int N, int K);
+size_t matmul_workspace_floats(const MatmulFwd& f);
 hipError_t matmul_fwd(const MatmulFwd& f, float* ws, hipStream_t stream);
-size_t matmul_backward_workspace_floats(int dt, long long M, int N, int K, bool dx, bool dw, bool db);
+size_t matmul_backward_workspace_floats(const MatmulBwd& f);
 hipError_t matmul_bwd(const MatmulBwd& f, float* ws, hipStream_t stream);
 
 // One AdamW step over tensors whose states are fp32 (bits 32) or 8-bit codes

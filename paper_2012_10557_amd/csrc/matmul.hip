@@ -36,6 +36,7 @@ template <typename T> struct MmArgs {
   const T *a, *b;
   long long lda, ldb;
   long long R, C, Tn;  // outputs along r and c, reduction length
+  long long Ra, Cb;    // outputs that a and b hold in memory (more than R and C in a padded copy)
   const float* bias;   // [R] or null
   const T* res;        // [C][R] or null
   long long ldr;
@@ -239,13 +240,13 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
     int x, u;
     if (q < OpA::UNITS) {
       OpA::place(q + lane, x, u);
-      const long long last = AOC ? max(0LL, a.R - (DMA ? OpA::E : 1)) : a.R - 1;
+      const long long last = AOC && DMA ? a.Ra - OpA::E : a.R - 1;
       const long long g = min(r0 + x, last), k = t_begin + u;
       src[j] = AOC ? a.a + k * a.lda + g : a.a + g * a.lda + k;
       whole[j] = AOC ? (int)min((long long)OpA::E, a.R - g) : OpA::E;
     } else {
       OpB::place(q - OpA::UNITS + lane, x, u);
-      const long long last = BOC ? max(0LL, a.C - (DMA ? OpB::E : 1)) : a.C - 1;
+      const long long last = BOC && DMA ? a.Cb - OpB::E : a.C - 1;
       const long long g = min(c0 + x, last), k = t_begin + u;
       src[j] = BOC ? a.b + k * a.ldb + g : a.b + g * a.ldb + k;
       whole[j] = BOC ? (int)min((long long)OpB::E, a.C - g) : OpB::E;
@@ -514,6 +515,7 @@ hipError_t mm_run(MmArgs<T> a, bool dma, hipStream_t st) {
     MmArgs<T> b = a;
     b.C = std::min(cs, C - c);
     b.b = a.b + (BOC ? c : c * a.ldb);
+    b.Cb = a.Cb - c;
     if (a.res) b.res = a.res + c * a.ldr;
     if (a.z) b.z = a.z + c * a.ldz;
     b.y = (OT*)a.y + c * a.ldy;
@@ -548,13 +550,82 @@ hipError_t mm_run(MmArgs<T> a, bool dma, hipStream_t st) {
   return hipSuccess;
 }
 
+// Rows of a matrix copied to whole units, the rest of the last one zero.
+template <typename T>
+__global__ __launch_bounds__(256) void mm_pack_kernel(const T* p, long long ld, long long rows, int cols,
+                                                      uint4* out) {
+  constexpr int E = Elt<T>::E;
+  const int units = cdiv(cols, E);
+  const long long i = (long long)blockIdx.x * 256 + threadIdx.x, r = i / units;
+  if (r >= rows) return;
+  const int u = (int)(i - r * units);
+  out[i] = load_any(p + r * ld + u * E, min(E, cols - u * E));
+}
+
+// An operand: `rows` rows of `cols` elements, ld apart.
+struct MmMat {
+  const void* p;
+  long long ld, rows;
+  int cols;
+  bool units(int dt) const { return cols % dtype_vec(dt) == 0 && unit16(p, ld, dt); }
+  int padded(int dt) const { return (int)cdivl(cols, dtype_vec(dt)) * dtype_vec(dt); }
+  size_t pack_floats(int dt) const { return ((size_t)rows * padded(dt) * dtype_size(dt) + 15) / 16 * 4; }
+};
+// Whether operands off 16 bytes are worth a padded copy.  Through registers a
+// bf16 product runs at about 300 TFLOP/s, with copies to LDS at 1100; a copied
+// element costs 4 bytes of traffic, so both directions of the result have to
+// be some hundreds long, and the product long enough for two more launches
+// (16384 x 2047 x 8192: 1812 us without).
+bool mm_pack(int dt, long long R, long long C, long long Tn) {
+  return dt == DT_BF16 && R * C >= 256 * (R + C) && (double)R * C * Tn >= 2e9;
+}
+template <typename T> hipError_t mm_copy(MmMat& m, float* ws, hipStream_t st) {
+  const int dt = sizeof(T) == 2 ? DT_BF16 : DT_F32;
+  const long long units = m.padded(dt) / Elt<T>::E, most = std::max(1LL, (1LL << 30) / units);
+  for (long long r = 0; r < m.rows; r += most) {
+    const long long n = std::min(most, m.rows - r);
+    hipLaunchKernelGGL(mm_pack_kernel<T>, dim3((unsigned)cdivl(n * units, 256)), dim3(256), 0, st,
+                       (const T*)m.p + r * m.ld, m.ld, n, m.cols, (uint4*)ws + r * units);
+    EKYA_HIP(hipGetLastError());
+  }
+  m.p = ws;
+  m.ld = m.cols = m.padded(dt);
+  return hipSuccess;
+}
+
+// D from operands A and B (AOC, BOC: with the reduction as rows); a: all but
+// the operands.
+template <typename T, typename OT, bool AOC, bool BOC, int ACT>
+hipError_t mm_product(MmArgs<T> a, const MmMat& A, const MmMat& B, hipStream_t st) {
+  const int dt = sizeof(T) == 2 ? DT_BF16 : DT_F32;
+  a.a = (const T*)A.p;
+  a.lda = A.ld;
+  a.b = (const T*)B.p;
+  a.ldb = B.ld;
+  a.Ra = A.cols;
+  a.Cb = B.cols;
+  return mm_run<T, OT, AOC, BOC, ACT>(a, A.units(dt) && B.units(dt), st);
+}
+
+size_t mm_forward_floats(const MatmulFwd& f) {
+  const MmMat x{f.x, f.ldx, f.M, f.K}, w{f.w, f.ldw, f.N, f.K};
+  size_t n = mm_part_floats(f.N, f.M, f.K, f.dt);
+  if (mm_pack(f.dt, f.N, f.M, f.K))
+    n += (x.units(f.dt) ? 0 : x.pack_floats(f.dt)) + (w.units(f.dt) ? 0 : w.pack_floats(f.dt));
+  return n;
+}
+
 template <typename T> hipError_t mm_forward(const MatmulFwd& f, float* ws, hipStream_t st) {
-  const int dt = sizeof(T) == 2 ? DT_BF16 : DT_F32, E = Elt<T>::E;
+  const int dt = sizeof(T) == 2 ? DT_BF16 : DT_F32;
+  MmMat x{f.x, f.ldx, f.M, f.K}, w{f.w, f.ldw, f.N, f.K};
+  if (mm_pack(dt, f.N, f.M, f.K))
+    for (MmMat* m : {&x, &w})
+      if (!m->units(dt)) {
+        const size_t n = m->pack_floats(dt);
+        EKYA_HIP(mm_copy<T>(*m, ws, st));
+        ws += n;
+      }
   MmArgs<T> a{};
-  a.a = (const T*)f.w;
-  a.lda = f.ldw;
-  a.b = (const T*)f.x;
-  a.ldb = f.ldx;
   a.R = f.N;
   a.C = f.M;
   a.Tn = f.K;
@@ -569,8 +640,7 @@ template <typename T> hipError_t mm_forward(const MatmulFwd& f, float* ws, hipSt
   a.part = ws;
   a.vec = unit16(f.y, f.ldy, dt) && (!f.z || unit16(f.z, f.ldz, dt)) &&
           (!f.res || unit16(f.res, f.ldr, dt)) && reinterpret_cast<uintptr_t>(f.bias) % 16 == 0;
-  const bool dma = f.K % E == 0 && unit16(f.w, f.ldw, dt) && unit16(f.x, f.ldx, dt);
-  return act_dispatch(f.act, [&](auto k) { return mm_run<T, T, false, false, k.value>(a, dma, st); });
+  return act_dispatch(f.act, [&](auto k) { return mm_product<T, T, false, false, k.value>(a, w, x, st); });
 }
 
 // ----------------------------------------------------------------- backward
@@ -673,6 +743,10 @@ size_t db_part_floats(long long M, int N, int E) {
 template <typename T, int E> hipError_t dz_run(DzArgs a, int act, float* db, hipStream_t st) {
   dz_cut(a, E);
   const long long chunks = cdivl(a.M, a.rows);
+  if (chunks == 1 && db) {
+    a.part = db;
+    db = nullptr;
+  }
   if (chunks) {
     EKYA_HIP(act_dispatch(act, [&](auto k) {
       hipLaunchKernelGGL((dz_kernel<T, E, k.value>), dim3((unsigned)(chunks * a.cchunks)), dim3(DZ_NT),
@@ -688,7 +762,7 @@ template <typename T, int E> hipError_t dz_run(DzArgs a, int act, float* db, hip
 }
 
 template <typename T> hipError_t mm_backward(const MatmulBwd& f, float* ws, hipStream_t st) {
-  const int dt = sizeof(T) == 2 ? DT_BF16 : DT_F32, E = Elt<T>::E;
+  const int dt = sizeof(T) == 2 ? DT_BF16 : DT_F32;
   const bool act = f.act != ACT_NONE;
   const void* dz = act ? f.dz : f.dy;
   const long long lddz = act ? f.lddz : f.lddy;
@@ -703,60 +777,79 @@ template <typename T> hipError_t mm_backward(const MatmulBwd& f, float* ws, hipS
     a.M = f.M;
     a.N = f.N;
     a.part = f.db ? ws : nullptr;
-    const bool unit = f.N % E == 0 && unit16(f.dy, f.lddy, dt) &&
+    const bool unit = f.N % Elt<T>::E == 0 && unit16(f.dy, f.lddy, dt) &&
                       (!act || (unit16(f.z, f.ldz, dt) && unit16(f.dz, f.lddz, dt)));
     EKYA_HIP(unit ? (dz_run<T, Elt<T>::E>(a, f.act, f.db, st)) : (dz_run<T, 1>(a, f.act, f.db, st)));
   }
+  MmMat g{dz, lddz, f.M, f.N};  // copied once for both products
+  const bool copy_dx = f.dx && mm_pack(dt, f.K, f.M, f.N), copy_dw = f.dw && mm_pack(dt, f.K, f.N, f.M);
+  MmMat packed = g;
+  if ((copy_dx || copy_dw) && f.M > 0 && !g.units(dt)) {
+    const size_t n = g.pack_floats(dt);
+    EKYA_HIP(mm_copy<T>(packed, ws, st));
+    ws += n;
+  }
+  auto other = [&](MmMat m, bool copy, float** rest, hipError_t* e) {
+    *rest = ws;
+    if (copy && !m.units(dt)) {
+      const size_t n = m.pack_floats(dt);
+      *e = mm_copy<T>(m, ws, st);
+      *rest = ws + n;
+    }
+    return m;
+  };
+  hipError_t e = hipSuccess;
   if (f.dx && f.M > 0) {
     MmArgs<T> a{};
-    a.a = (const T*)f.w;
-    a.lda = f.ldw;
-    a.b = (const T*)dz;
-    a.ldb = lddz;
+    const MmMat w = other({f.w, f.ldw, f.N, f.K}, copy_dx, &a.part, &e);
+    EKYA_HIP(e);
     a.R = f.K;
     a.C = f.M;
     a.Tn = f.N;
     a.y = f.dx;
     a.ldy = f.lddx;
-    a.part = ws;
     a.vec = unit16(f.dx, f.lddx, dt);
-    const bool dma = f.K % E == 0 && f.N % E == 0 && unit16(f.w, f.ldw, dt) && unit16(dz, lddz, dt);
-    EKYA_HIP((mm_run<T, T, true, false, ACT_NONE>(a, dma, st)));
+    EKYA_HIP((mm_product<T, T, true, false, ACT_NONE>(a, w, copy_dx ? packed : g, st)));
   }
   if (f.dw) {
     MmArgs<T> a{};
-    a.a = (const T*)f.x;
-    a.lda = f.ldx;
-    a.b = (const T*)dz;
-    a.ldb = lddz;
+    const MmMat x = other({f.x, f.ldx, f.M, f.K}, copy_dw && f.M > 0, &a.part, &e);
+    EKYA_HIP(e);
     a.R = f.K;
     a.C = f.N;
     a.Tn = f.M;
     a.y = f.dw;
     a.ldy = f.K;
-    a.part = ws;
     const bool low = dt == DT_BF16 && f.dw_dt == DT_BF16;
     a.vec = unit16(f.dw, f.K, low ? DT_BF16 : DT_F32);
-    const bool dma = f.K % E == 0 && f.N % E == 0 && unit16(f.x, f.ldx, dt) && unit16(dz, lddz, dt);
-    EKYA_HIP(low ? (mm_run<T, T, true, true, ACT_NONE>(a, dma, st))
-                 : (mm_run<T, float, true, true, ACT_NONE>(a, dma, st)));
+    const MmMat& b = copy_dw && f.M > 0 ? packed : g;
+    EKYA_HIP(low ? (mm_product<T, T, true, true, ACT_NONE>(a, x, b, st))
+                 : (mm_product<T, float, true, true, ACT_NONE>(a, x, b, st)));
   }
   return hipSuccess;
 }
 
+size_t mm_backward_floats(const MatmulBwd& f) {
+  const bool act = f.act != ACT_NONE;
+  const MmMat g{act ? f.dz : f.dy, act ? f.lddz : f.lddy, f.M, f.N}, x{f.x, f.ldx, f.M, f.K},
+      w{f.w, f.ldw, f.N, f.K};
+  const int dt = f.dt, E = dtype_vec(dt);
+  const bool copy_dx = f.dx && mm_pack(dt, f.K, f.M, f.N), copy_dw = f.dw && mm_pack(dt, f.K, f.N, f.M);
+  size_t n = 0, db = 0;
+  if (f.dx)
+    n = mm_part_floats(f.K, f.M, f.N, dt) + (copy_dx && !w.units(dt) ? w.pack_floats(dt) : 0);
+  if (f.dw)
+    n = std::max(n, mm_part_floats(f.K, f.N, f.M, dt) + (copy_dw && !x.units(dt) ? x.pack_floats(dt) : 0));
+  if ((copy_dx || copy_dw) && !g.units(dt)) n += g.pack_floats(dt);
+  // the bias gradient's partial sums are done with before the products begin
+  if (f.db) db = std::max(db_part_floats(f.M, f.N, 1), f.N % E == 0 ? db_part_floats(f.M, f.N, E) : 0);
+  return std::max(n, db);
+}
+
 }  // namespace
 
-size_t matmul_workspace_floats(int dt, long long M, int N, int K) {
-  return mm_part_floats(N, M, K, dt);
-}
-
-size_t matmul_backward_workspace_floats(int dt, long long M, int N, int K, bool dx, bool dw, bool db) {
-  size_t f = 0;
-  if (db) f = std::max(db_part_floats(M, N, 1), N % dtype_vec(dt) == 0 ? db_part_floats(M, N, dtype_vec(dt)) : 0);
-  if (dx) f = std::max(f, mm_part_floats(K, M, N, dt));
-  if (dw) f = std::max(f, mm_part_floats(K, N, M, dt));
-  return f;
-}
+size_t matmul_workspace_floats(const MatmulFwd& f) { return mm_forward_floats(f); }
+size_t matmul_backward_workspace_floats(const MatmulBwd& f) { return mm_backward_floats(f); }
 
 hipError_t matmul_fwd(const MatmulFwd& f, float* ws, hipStream_t st) {
   return f.dt == DT_BF16 ? mm_forward<bf16>(f, ws, st) : mm_forward<float>(f, ws, st);

@@ -246,3 +246,15 @@ def test_matmul_in_a_graph_repeats_the_eager_result(M, N, K):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, eager)), i
+
+
+@pytest.mark.parametrize("M,N,K,pad,offset", [(1500, 1030, 1411, 0, 0), (1504, 1032, 1411, 0, 0),
+                                              (1504, 1030, 1408, 5, 3), (1504, 1032, 1408, 3, 1)])
+def test_large_operands_off_16_bytes(M, N, K, pad, offset):
+    """Products long enough for padded copies of what does not lie on 16 bytes: all operands, x and w
+    only, dz only, or by their rows' distance; what lies between the rows is NaN."""
+    import torch
+    c = Case(M, N, K, torch.bfloat16, pad, offset)
+    check_forward(c, "silu", True, True, False, True)
+    check_backward(c, "gelu", torch.float32)
+    check_backward(c, "none", torch.bfloat16)
