@@ -479,7 +479,7 @@ struct MmPlan {
 //
 // With less than 192 tiles of 128 most CUs hold one block or none: 64 x 64, and
 // the reduction split until 512 blocks run, a part 16 stages long at least (6
-// in fp32, whose stages take longer).  128 against 64: 1000^3 14.8 and 9.2 us,
+// in fp32 and 4 without DMA, whose stages take longer).  128 against 64: 1000^3 14.8 and 9.2 us,
 // 512^3 10.3 and 6.0, but with 256 tiles of 128 2048^3 27.4 and 28.0; parts of
 // 32, 16 and 8 stages: 1024 x 512 x 4096 21.6, 17.5 and 19.2.
 MmPlan mm_plan(long long R, long long C, long long Tn, int dt, bool dma) {
@@ -490,13 +490,13 @@ MmPlan mm_plan(long long R, long long C, long long Tn, int dt, bool dma) {
     return {256, 1, (int)ns};
   if (t128 >= 192) return {128, 1, (int)ns};
   const long long t64 = std::max(1LL, cdivl(R, 64) * cdivl(C, 64));
-  const long long want = std::max(1LL, std::min(512 / t64, ns / (dt == DT_BF16 ? 16 : 6)));
+  const long long want = std::max(1LL, std::min(512 / t64, ns / (!dma ? 4 : dt == DT_BF16 ? 16 : 6)));
   const int stages = (int)cdivl(ns, want);
   return {64, (int)cdivl(ns, stages), stages};
 }
 long long round4(long long n) { return (n + 3) & ~3LL; }
-size_t mm_part_floats(long long R, long long C, long long Tn, int dt) {
-  const MmPlan p = mm_plan(R, C, Tn, dt, false);
+size_t mm_part_floats(long long R, long long C, long long Tn, int dt, bool dma) {
+  const MmPlan p = mm_plan(R, C, Tn, dt, dma);
   return p.splits > 1 ? (size_t)p.splits * C * round4(R) : 0;
 }
 
@@ -609,8 +609,9 @@ hipError_t mm_product(MmArgs<T> a, const MmMat& A, const MmMat& B, hipStream_t s
 
 size_t mm_forward_floats(const MatmulFwd& f) {
   const MmMat x{f.x, f.ldx, f.M, f.K}, w{f.w, f.ldw, f.N, f.K};
-  size_t n = mm_part_floats(f.N, f.M, f.K, f.dt);
-  if (mm_pack(f.dt, f.N, f.M, f.K))
+  const bool copy = mm_pack(f.dt, f.N, f.M, f.K);
+  size_t n = mm_part_floats(f.N, f.M, f.K, f.dt, copy || (x.units(f.dt) && w.units(f.dt)));
+  if (copy)
     n += (x.units(f.dt) ? 0 : x.pack_floats(f.dt)) + (w.units(f.dt) ? 0 : w.pack_floats(f.dt));
   return n;
 }
@@ -837,9 +838,9 @@ size_t mm_backward_floats(const MatmulBwd& f) {
   const bool copy_dx = f.dx && mm_pack(dt, f.K, f.M, f.N), copy_dw = f.dw && mm_pack(dt, f.K, f.N, f.M);
   size_t n = 0, db = 0;
   if (f.dx)
-    n = mm_part_floats(f.K, f.M, f.N, dt) + (copy_dx && !w.units(dt) ? w.pack_floats(dt) : 0);
+    n = mm_part_floats(f.K, f.M, f.N, dt, copy_dx || (w.units(dt) && g.units(dt))) + (copy_dx && !w.units(dt) ? w.pack_floats(dt) : 0);
   if (f.dw)
-    n = std::max(n, mm_part_floats(f.K, f.N, f.M, dt) + (copy_dw && !x.units(dt) ? x.pack_floats(dt) : 0));
+    n = std::max(n, mm_part_floats(f.K, f.N, f.M, dt, copy_dw || (x.units(dt) && g.units(dt))) + (copy_dw && !x.units(dt) ? x.pack_floats(dt) : 0));
   if ((copy_dx || copy_dw) && !g.units(dt)) n += g.pack_floats(dt);
   // the bias gradient's partial sums are done with before the products begin
   if (f.db) db = std::max(db_part_floats(f.M, f.N, 1), f.N % E == 0 ? db_part_floats(f.M, f.N, E) : 0);
