@@ -207,9 +207,9 @@ __device__ __forceinline__ void mm_tile_of(int L, int tiles_r, int tiles_c, int&
 
 // BR x BC tile, WR x WC waves.  DMA: both operands are read in whole units on
 // 16 bytes (global memory to LDS directly); else through registers.
-template <typename T, typename OT, int BR, int BC, int WR, int WC, bool AOC, bool BOC, bool DMA, int ACT>
+template <typename T, typename OT, int BR, int BC, int WR, int WC, int NST, bool AOC, bool BOC, bool DMA, int ACT>
 __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
-  constexpr int NW = WR * WC, NST = 2;
+  constexpr int NW = WR * WC;
   constexpr int TI = BR / WR / 16, TJ = BC / WC / 16;
   static_assert(TI % 4 == 0, "64 outputs of A at a time");
   using OpA = MmOperand<T, BR, AOC>;
@@ -318,9 +318,10 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
   // one visible and frees its buffer; read the next one's first half and
   // multiply the second.
   if constexpr (DMA) {
-    if (ns > 0) copy(0);
-    if (ns > 1) copy(1);
-    if (ns > 1) wait_vmcnt<LPS>(); else wait_vmcnt<0>();
+#pragma unroll
+    for (int p = 0; p < NST; ++p)
+      if (p < ns) copy(p);
+    if (ns >= NST) wait_vmcnt<LPS*(NST - 1)>(); else wait_vmcnt<0>();
   } else {
     fetch(0);
     put(0);
@@ -335,10 +336,10 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
   int s = 0;
   if constexpr (DMA) {  // without a branch while whole stages follow
     const int full = (int)((t_end - t_begin) / TS);
-    for (; s + 2 < full; ++s) {
+    for (; s + NST < full; ++s) {
       frags(s, 1);
       mma_tile(acc, fa[0], fb[0], (T*)nullptr);
-      wait_vmcnt<0>();
+      wait_vmcnt<LPS*(NST - 2)>();
       mm_barrier();
       copy_full(s);
       frags(s + 1, 0);
@@ -348,10 +349,12 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
   for (; s < ns; ++s) {
     frags(s, 1);
     mma_tile(acc, fa[0], fb[0], (T*)nullptr);
-    if constexpr (DMA) wait_vmcnt<0>();
+    if constexpr (DMA) {
+      if (s + NST - 1 < ns) wait_vmcnt<LPS*(NST - 2)>(); else wait_vmcnt<0>();
+    }
     mm_barrier();
     if constexpr (DMA) {
-      if (s + 2 < ns) copy(s + 2);
+      if (s + NST < ns) copy(s + NST);
     } else {
       if (s + 2 < ns) put(s + 2);
       if (s + 3 < ns) fetch(s + 3);
@@ -370,7 +373,7 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
   const int cols = (int)min((long long)TJ * 16, a.C - cw);
   float* part = a.part + split * a.C * a.Rp;
   f32x4* own = reinterpret_cast<f32x4*>(smem) + wave * 16 * TJ * 16;
-  static_assert(NW * TJ * 16 * 64 * 4 <= sizeof(smem), "64 rows of every wave");
+  static_assert(NW * TJ * 16 * 64 * 4 <= (int)sizeof(smem), "64 rows of every wave");
 #pragma unroll
   for (int g = 0; g < TI / 4; ++g) {
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the wave's own accesses, in order
@@ -478,10 +481,13 @@ struct MmPlan {
 // 31.1, 2048^3 (64 tiles of 256) 53.6 and 27.4.
 //
 // With less than 192 tiles of 128 most CUs hold one block or none: 64 x 64, and
-// the reduction split until 512 blocks run, a part 16 stages long at least (6
-// in fp32 and 4 without DMA, whose stages take longer).  128 against 64: 1000^3 14.8 and 9.2 us,
-// 512^3 10.3 and 6.0, but with 256 tiles of 128 2048^3 27.4 and 28.0; parts of
-// 32, 16 and 8 stages: 1024 x 512 x 4096 21.6, 17.5 and 19.2.
+// the reduction split until 512 blocks run where a part is still 32 stages
+// long, else until 256 do (one a CU, three stages in flight).  128 against 64:
+// 1000^3 14.8 and 9.2 us, 512^3 10.3 and 6.0, but with 256 tiles of 128 2048^3
+// 27.4 and 28.0.  256 against 512 blocks: 128 x 2048 x 8192 (parts of 32 and 16
+// stages) 12.6 and 15.7, 256 x 1024 x 25088 (98 and 49) 40.6 and 33.4.  A part has
+// 16 stages at least (1024 x 512 x 4096 in parts of 32, 16 and 8: 21.6, 17.5 and
+// 19.2), 6 in fp32 and 4 without DMA, whose stages take longer.
 MmPlan mm_plan(long long R, long long C, long long Tn, int dt, bool dma) {
   const long long ns = std::max(1LL, cdivl(Tn, 8 * dtype_vec(dt)));
   const long long t256 = cdivl(R, 256) * cdivl(C, 256), t128 = cdivl(R, 128) * cdivl(C, 128);
@@ -490,7 +496,8 @@ MmPlan mm_plan(long long R, long long C, long long Tn, int dt, bool dma) {
     return {256, 1, (int)ns};
   if (t128 >= 192) return {128, 1, (int)ns};
   const long long t64 = std::max(1LL, cdivl(R, 64) * cdivl(C, 64));
-  const long long want = std::max(1LL, std::min(512 / t64, ns / (!dma ? 4 : dt == DT_BF16 ? 16 : 6)));
+  const long long blocks = !dma || dt != DT_BF16 || ns * t64 >= 512 * 32 ? 512 : 256;
+  const long long want = std::max(1LL, std::min(blocks / t64, ns / (!dma ? 4 : dt == DT_BF16 ? 16 : 6)));
   const int stages = (int)cdivl(ns, want);
   return {64, (int)cdivl(ns, stages), stages};
 }
@@ -522,20 +529,28 @@ hipError_t mm_run(MmArgs<T> a, bool dma, hipStream_t st) {
     b.tiles_r = (int)tiles_r;
     b.tiles_c = (int)cdivl(b.C, p.tile);
     const dim3 grid((unsigned)((long long)b.tiles_r * b.tiles_c * b.splits));
-    auto go = [&](auto tile, auto wr, auto wc, auto direct) {
-      hipLaunchKernelGGL((mm_kernel<T, OT, tile.value, tile.value, wr.value, wc.value, AOC, BOC, direct.value, ACT>),
+    auto go = [&](auto tile, auto wr, auto wc, auto nst, auto direct) {
+      hipLaunchKernelGGL((mm_kernel<T, OT, tile.value, tile.value, wr.value, wc.value, nst.value, AOC, BOC,
+                                    direct.value, ACT>),
                          grid, dim3(wr.value * wc.value * 64), 0, st, b);
     };
-    using std::integral_constant;
-    using I1 = integral_constant<int, 1>;
-    using I2 = integral_constant<int, 2>;
-    using I4 = integral_constant<int, 4>;
+    using I1 = std::integral_constant<int, 1>;
+    using I2 = std::integral_constant<int, 2>;
+    using I3 = std::integral_constant<int, 3>;
+    using I4 = std::integral_constant<int, 4>;
+    using T64 = std::integral_constant<int, 64>;
+    using T128 = std::integral_constant<int, 128>;
+    using T256 = std::integral_constant<int, 256>;
     if constexpr (sizeof(T) == 2)
-      if (p.tile == 256) go(integral_constant<int, 256>{}, I2{}, I4{}, std::true_type{});
-    if (p.tile == 128 && dma) go(integral_constant<int, 128>{}, I2{}, I2{}, std::true_type{});
-    if (p.tile == 128 && !dma) go(integral_constant<int, 128>{}, I2{}, I2{}, std::false_type{});
-    if (p.tile == 64 && dma) go(integral_constant<int, 64>{}, I1{}, I4{}, std::true_type{});
-    if (p.tile == 64 && !dma) go(integral_constant<int, 64>{}, I1{}, I4{}, std::false_type{});
+      if (p.tile == 256) go(T256{}, I2{}, I4{}, I2{}, std::true_type{});
+    if (p.tile == 128 && dma) go(T128{}, I2{}, I2{}, I2{}, std::true_type{});
+    if (p.tile == 128 && !dma) go(T128{}, I2{}, I2{}, I2{}, std::false_type{});
+    // a CU's only block keeps three stages in flight (128 x 2048 x 8192: 18.6 us
+    // with two, 12.6 with three); where it has more, two buffers leave them room
+    // (1024 x 4096 x 512 with 512 tiles: 13.0 and 14.1 us)
+    if (p.tile == 64 && dma && grid.x <= 256) go(T64{}, I1{}, I4{}, I3{}, std::true_type{});
+    if (p.tile == 64 && dma && grid.x > 256) go(T64{}, I1{}, I4{}, I2{}, std::true_type{});
+    if (p.tile == 64 && !dma) go(T64{}, I1{}, I4{}, I2{}, std::false_type{});
     EKYA_HIP(hipGetLastError());
   }
   if (a.splits > 1) {
