@@ -284,8 +284,9 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
     for (int j = 0; j < LPS; ++j)
       dma16(there(j, left) ? (const void*)src[j] : zero, slot + (wave + NW * j) * 64);
   };
-  uint4 held[LPS];  // without DMA: a stage on its way
-  auto fetch = [&](int s) {
+  constexpr int H = BR == 64 ? 2 : 1;  // without DMA: stages on their way in registers
+  uint4 held[H][LPS];
+  auto fetch = [&](int s, uint4 (&held)[LPS]) {
     const int left = left_at(s);
 #pragma unroll
     for (int j = 0; j < LPS; ++j) {
@@ -293,7 +294,7 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
       src[j] += (wave + NW * j) * 64 < OpA::UNITS ? step_a : step_b;
     }
   };
-  auto put = [&](int s) {
+  auto put = [&](int s, uint4 (&held)[LPS]) {
     uint4* slot = smem + (s % NST) * SU;
 #pragma unroll
     for (int j = 0; j < LPS; ++j) slot[(wave + NW * j) * 64 + lane] = held[j];
@@ -323,13 +324,15 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
       if (p < ns) copy(p);
     if (ns >= NST) wait_vmcnt<LPS*(NST - 1)>(); else wait_vmcnt<0>();
   } else {
-    fetch(0);
-    put(0);
+    fetch(0, held[0]);
+    put(0, held[0]);
     if (ns > 1) {
-      fetch(1);
-      put(1);
+      fetch(1, held[0]);
+      put(1, held[0]);
     }
-    if (ns > 2) fetch(2);
+#pragma unroll
+    for (int h = 0; h < H; ++h)
+      if (2 + h < ns) fetch(2 + h, held[h]);
   }
   mm_barrier();
   frags(0, 0);
@@ -346,7 +349,7 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
       mma_tile(acc, fa[1], fb[1], (T*)nullptr);
     }
   }
-  for (; s < ns; ++s) {
+  auto step = [&](int s, uint4 (&held)[LPS]) {
     frags(s, 1);
     mma_tile(acc, fa[0], fb[0], (T*)nullptr);
     if constexpr (DMA) {
@@ -356,11 +359,16 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
     if constexpr (DMA) {
       if (s + NST < ns) copy(s + NST);
     } else {
-      if (s + 2 < ns) put(s + 2);
-      if (s + 3 < ns) fetch(s + 3);
+      if (s + 2 < ns) put(s + 2, held);
+      if (s + 2 + H < ns) fetch(s + 2 + H, held);
     }
     frags(s + 1, 0);  // after the last stage: not used
     mma_tile(acc, fa[1], fb[1], (T*)nullptr);
+  };
+  for (; s < ns; s += H) {
+    step(s, held[0]);
+    if constexpr (H == 2)
+      if (s + 1 < ns) step(s + 1, held[1]);
   }
 
   // 64 rows of the wave's tile at a time pass through its own part of LDS (no
