@@ -120,8 +120,8 @@ __device__ __forceinline__ uint2 mm_read_tr(const char* p) {
 // LDS layout of a stage.  Rows of t-contiguous operands are 8 units of 16
 // bytes; unit u of row r is stored at u ^ f(r).  Operands with t as rows keep
 // their rows of BX outputs; unit u of row t is stored at u ^ h(t).  f and h
-// spread what 8 (16-byte reads) or 16 (8-byte reads) consecutive lanes touch
-// over all banks.
+// spread what 8 (16-byte reads) or 32 (8-byte reads) consecutive lanes touch
+// over all 64 banks.
 template <typename T, int BX, bool OC> struct MmOperand {
   static constexpr int E = Elt<T>::E;
   static constexpr int TS = 8 * E;               // reduction elements of a stage
@@ -130,7 +130,9 @@ template <typename T, int BX, bool OC> struct MmOperand {
   static __device__ __forceinline__ int swizzle(int row) {
     if constexpr (!OC) return row & 7;
     if constexpr (sizeof(T) == 4) return ((row >> 2) & 3) << 2;
-    return (row & 3) << 1;
+    // 32 lanes read 32 bytes of each of rows 0 .. 3 and 8 .. 11 (and 16 on)
+    if constexpr (BX == 64) return ((row >> 1) & 1) << 2 | ((row >> 3) & 1) << 1;  // rows of 128 bytes
+    return (row & 3) << 1 | ((row >> 3) & 1) << 3;
   }
   // Where the unit stored at position q of a stage comes from: output x (of
   // the tile) and reduction element t (of the stage).
@@ -192,23 +194,27 @@ template <typename T> __device__ __forceinline__ uint4 load_any(const T* p, int 
   return t.u;
 }
 
-// Workgroups go round the 8 XCDs; each XCD gets a contiguous range of tiles,
-// and a range walks the tiles four rows at a time, so that the blocks an XCD
-// runs together share panels of both operands in its L2.
-__device__ __forceinline__ void mm_tile_of(int L, int tiles_r, int tiles_c, int& tr, int& tc) {
-  const int total = tiles_r * tiles_c;
+// Workgroups go round the 8 XCDs; each XCD gets a contiguous range of (split,
+// tile) items, whole splits where there are some (their tiles read the same
+// part of both operands), and a range walks the tiles four rows at a time, so
+// that the blocks an XCD runs together share panels of both operands in its L2.
+__device__ __forceinline__ void mm_item(int L, int tiles_r, int tiles_c, int splits, int& split, int& tr, int& tc) {
+  const int tiles = tiles_r * tiles_c, total = tiles * splits;
   const int x = L & 7, k = L >> 3;
-  const int t = x * (total >> 3) + min(x, total & 7) + k;
+  const int item = x * (total >> 3) + min(x, total & 7) + k;
+  split = item / tiles;
+  const int t = item - split * tiles;
   const int band = t / (4 * tiles_c), rest = t - band * 4 * tiles_c;
   const int h = min(4, tiles_r - 4 * band);
   tc = rest / h;
   tr = 4 * band + rest - tc * h;
 }
 
-// BR x BC tile, WR x WC waves.  DMA: both operands are read in whole units on
+// BR x BC tile, WR x WC waves, KG groups of them with a part of the reduction
+// each (buffers of their own, sums added up at the end).  DMA: both operands are read in whole units on
 // 16 bytes (global memory to LDS directly); else through registers.
-template <typename T, typename OT, int BR, int BC, int WR, int WC, int NST, bool AOC, bool BOC, bool DMA, int ACT>
-__global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
+template <typename T, typename OT, int BR, int BC, int WR, int WC, int NST, int KG, bool AOC, bool BOC, bool DMA, int ACT>
+__global__ __launch_bounds__(WR* WC* KG * 64, 2) void mm_kernel(MmArgs<T> a) {
   constexpr int NW = WR * WC;
   constexpr int TI = BR / WR / 16, TJ = BC / WC / 16;
   static_assert(TI % 4 == 0, "64 outputs of A at a time");
@@ -217,18 +223,21 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
   constexpr int TS = OpA::TS, SU = OpA::UNITS + OpB::UNITS;
   constexpr int LPS = SU / 64 / NW;  // units of a lane in a stage
   static_assert(OpA::UNITS % 64 == 0 && SU % (64 * NW) == 0, "whole copies");
-  __shared__ uint4 smem[NST * SU];
+  __shared__ uint4 buffers[KG * NST * SU];
 
   const int lane = threadIdx.x & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int tiles = a.tiles_r * a.tiles_c;
-  const int split = blockIdx.x / tiles;
-  int tr, tc;
-  mm_tile_of(blockIdx.x - split * tiles, a.tiles_r, a.tiles_c, tr, tc);
+  const int group = KG > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) / NW : 0;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) - group * NW;
+  uint4* const smem = buffers + group * NST * SU;
+  int split, tr, tc;
+  mm_item(blockIdx.x, a.tiles_r, a.tiles_c, a.splits, split, tr, tc);
   const long long r0 = (long long)tr * BR, c0 = (long long)tc * BC;
-  const long long t_begin = (long long)split * a.stages * TS;
-  const long long t_end = min(a.Tn, t_begin + (long long)a.stages * TS);
+  const long long part_t = (long long)a.stages * TS;  // reduction elements of a group
+  const long long t_first = split * KG * part_t;      // the block's
+  const long long t_begin = min(a.Tn, t_first + group * part_t), t_end = min(a.Tn, t_begin + part_t);
   const int ns = (int)cdivl(t_end - t_begin, TS);
+  // all groups meet at the barriers of the first, which has the most stages
+  const int most = KG > 1 ? (int)cdivl(min(a.Tn, t_first + part_t) - t_first, TS) : ns;
 
   // This lane's sources of the next stage.  Outputs past the end read what the
   // last one reads: their results are not stored.
@@ -338,7 +347,11 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
   frags(0, 0);
   int s = 0;
   if constexpr (DMA) {  // without a branch while whole stages follow
-    const int full = (int)((t_end - t_begin) / TS);
+    int full = (int)((t_end - t_begin) / TS);  // of the last group, which has the fewest
+    if constexpr (KG > 1) {
+      const long long l = min(a.Tn, t_first + (KG - 1) * part_t);
+      full = (int)((min(a.Tn, l + part_t) - l) / TS);
+    }
     for (; s + NST < full; ++s) {
       frags(s, 1);
       mma_tile(acc, fa[0], fb[0], (T*)nullptr);
@@ -350,8 +363,11 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
     }
   }
   auto step = [&](int s, uint4 (&held)[LPS]) {
-    frags(s, 1);
-    mma_tile(acc, fa[0], fb[0], (T*)nullptr);
+    const bool any = KG == 1 || s < ns;
+    if (any) {
+      frags(s, 1);
+      mma_tile(acc, fa[0], fb[0], (T*)nullptr);
+    }
     if constexpr (DMA) {
       if (s + NST - 1 < ns) wait_vmcnt<LPS*(NST - 2)>(); else wait_vmcnt<0>();
     }
@@ -362,13 +378,32 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
       if (s + 2 < ns) put(s + 2, held);
       if (s + 2 + H < ns) fetch(s + 2 + H, held);
     }
-    frags(s + 1, 0);  // after the last stage: not used
-    mma_tile(acc, fa[1], fb[1], (T*)nullptr);
+    if (any) {
+      frags(s + 1, 0);  // after the last stage: not used
+      mma_tile(acc, fa[1], fb[1], (T*)nullptr);
+    }
   };
-  for (; s < ns; s += H) {
+  for (; s < most; s += H) {
     step(s, held[0]);
     if constexpr (H == 2)
       if (s + 1 < ns) step(s + 1, held[1]);
+  }
+  if constexpr (KG > 1) {  // the first group adds the others' sums in their order
+    static_assert(DMA && NW * TI * TJ * 64 <= NST * SU, "a group's sums fit its buffers");
+    f32x4* sums = reinterpret_cast<f32x4*>(smem) + wave * TI * TJ * 64 + lane;
+    mm_barrier();
+    if (group > 0)
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) sums[(i * TJ + j) * 64] = acc[i][j];
+    mm_barrier();
+    if (group > 0) return;
+    for (int g = 1; g < KG; ++g)
+#pragma unroll
+      for (int i = 0; i < TI; ++i)
+#pragma unroll
+        for (int j = 0; j < TJ; ++j) acc[i][j] += sums[g * NST * SU + (i * TJ + j) * 64];
   }
 
   // 64 rows of the wave's tile at a time pass through its own part of LDS (no
@@ -381,7 +416,7 @@ __global__ __launch_bounds__(WR* WC * 64, 2) void mm_kernel(MmArgs<T> a) {
   const int cols = (int)min((long long)TJ * 16, a.C - cw);
   float* part = a.part + split * a.C * a.Rp;
   f32x4* own = reinterpret_cast<f32x4*>(smem) + wave * 16 * TJ * 16;
-  static_assert(NW * TJ * 16 * 64 * 4 <= (int)sizeof(smem), "64 rows of every wave");
+  static_assert(NW * TJ * 16 * 64 * 4 <= NST * SU * 16, "64 rows of every wave");
 #pragma unroll
   for (int g = 0; g < TI / 4; ++g) {
     __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the wave's own accesses, in order
@@ -477,7 +512,8 @@ bool unit16(const void* p, long long ld, int dt) {
 
 struct MmPlan {
   int tile;            // outputs of a tile in either direction
-  int splits, stages;  // stages of a split
+  int splits, stages;  // stages of a split (of a group of waves)
+  int groups;          // of waves in a block
 };
 // Which tile, and into how many parts the reduction is split.
 //
@@ -501,13 +537,17 @@ MmPlan mm_plan(long long R, long long C, long long Tn, int dt, bool dma) {
   const long long t256 = cdivl(R, 256) * cdivl(C, 256), t128 = cdivl(R, 128) * cdivl(C, 128);
   if (dma && dt == DT_BF16 && t256 >= 192 &&
       cdivl(t256, 256) * (10 + 1.58 * ns) <= 5 + t128 / 256. * (2.3 + 0.46 * ns))
-    return {256, 1, (int)ns};
-  if (t128 >= 192) return {128, 1, (int)ns};
+    return {256, 1, (int)ns, 1};
+  if (dma && dt == DT_BF16 && std::min(R, C) >= 128 && t128 <= 256 && ns * t128 >= 512 * 8) {
+    const long long parts = 2 * (256 / t128), stages = cdivl(ns, parts);
+    return {128, (int)cdivl(ns, 2 * stages), (int)stages, 2};
+  }
+  if (t128 >= 192) return {128, 1, (int)ns, 1};
   const long long t64 = std::max(1LL, cdivl(R, 64) * cdivl(C, 64));
   const long long blocks = !dma || dt != DT_BF16 || ns * t64 >= 512 * 32 ? 512 : 256;
   const long long want = std::max(1LL, std::min(blocks / t64, ns / (!dma ? 4 : dt == DT_BF16 ? 16 : 6)));
   const int stages = (int)cdivl(ns, want);
-  return {64, (int)cdivl(ns, stages), stages};
+  return {64, (int)cdivl(ns, stages), stages, 1};
 }
 long long round4(long long n) { return (n + 3) & ~3LL; }
 size_t mm_part_floats(long long R, long long C, long long Tn, int dt, bool dma) {
@@ -537,10 +577,10 @@ hipError_t mm_run(MmArgs<T> a, bool dma, hipStream_t st) {
     b.tiles_r = (int)tiles_r;
     b.tiles_c = (int)cdivl(b.C, p.tile);
     const dim3 grid((unsigned)((long long)b.tiles_r * b.tiles_c * b.splits));
-    auto go = [&](auto tile, auto wr, auto wc, auto nst, auto direct) {
-      hipLaunchKernelGGL((mm_kernel<T, OT, tile.value, tile.value, wr.value, wc.value, nst.value, AOC, BOC,
-                                    direct.value, ACT>),
-                         grid, dim3(wr.value * wc.value * 64), 0, st, b);
+    auto go = [&](auto tile, auto wr, auto wc, auto nst, auto kg, auto direct) {
+      hipLaunchKernelGGL((mm_kernel<T, OT, tile.value, tile.value, wr.value, wc.value, nst.value, kg.value, AOC,
+                                    BOC, direct.value, ACT>),
+                         grid, dim3(wr.value * wc.value * kg.value * 64), 0, st, b);
     };
     using I1 = std::integral_constant<int, 1>;
     using I2 = std::integral_constant<int, 2>;
@@ -550,15 +590,17 @@ hipError_t mm_run(MmArgs<T> a, bool dma, hipStream_t st) {
     using T128 = std::integral_constant<int, 128>;
     using T256 = std::integral_constant<int, 256>;
     if constexpr (sizeof(T) == 2)
-      if (p.tile == 256) go(T256{}, I2{}, I4{}, I2{}, std::true_type{});
-    if (p.tile == 128 && dma) go(T128{}, I2{}, I2{}, I2{}, std::true_type{});
-    if (p.tile == 128 && !dma) go(T128{}, I2{}, I2{}, I2{}, std::false_type{});
+      if (p.tile == 256) go(T256{}, I2{}, I4{}, I2{}, I1{}, std::true_type{});
+    if constexpr (sizeof(T) == 2)
+      if (p.tile == 128 && p.groups == 2) go(T128{}, I2{}, I2{}, I2{}, I2{}, std::true_type{});
+    if (p.tile == 128 && p.groups == 1 && dma) go(T128{}, I2{}, I2{}, I2{}, I1{}, std::true_type{});
+    if (p.tile == 128 && !dma) go(T128{}, I2{}, I2{}, I2{}, I1{}, std::false_type{});
     // a CU's only block keeps three stages in flight (128 x 2048 x 8192: 18.6 us
     // with two, 12.6 with three); where it has more, two buffers leave them room
     // (1024 x 4096 x 512 with 512 tiles: 13.0 and 14.1 us)
-    if (p.tile == 64 && dma && grid.x <= 256) go(T64{}, I1{}, I4{}, I3{}, std::true_type{});
-    if (p.tile == 64 && dma && grid.x > 256) go(T64{}, I1{}, I4{}, I2{}, std::true_type{});
-    if (p.tile == 64 && !dma) go(T64{}, I1{}, I4{}, I2{}, std::false_type{});
+    if (p.tile == 64 && dma && grid.x <= 256) go(T64{}, I1{}, I4{}, I3{}, I1{}, std::true_type{});
+    if (p.tile == 64 && dma && grid.x > 256) go(T64{}, I1{}, I4{}, I2{}, I1{}, std::true_type{});
+    if (p.tile == 64 && !dma) go(T64{}, I1{}, I4{}, I2{}, I1{}, std::false_type{});
     EKYA_HIP(hipGetLastError());
   }
   if (a.splits > 1) {
