@@ -686,10 +686,10 @@ void gn_cut(GnArgs& a, int E) {
 
 bool unit_ok(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
 
-// Launches `kernel` over samples of a.N in groups whose grids stay below 2^23
-// blocks; `per` blocks a sample.
+// Calls `go` over the samples in groups whose grids stay below 2^21 blocks (2^31
+// threads); `per` blocks a sample.
 template <typename F> hipError_t gn_samples(GnArgs a, size_t esize, long long per, F&& go) {
-  const long long most = std::max<long long>(1, (1 << 23) / per), N = a.N;
+  const long long most = std::max<long long>(8, (1 << 21) / per / 8 * 8), N = a.N;
   for (long long n = 0; n < N; n += most) {
     GnArgs b = a;
     b.N = (int)std::min(most, N - n);

@@ -25,9 +25,13 @@ __device__ __align__(16) uint4 g_mm_zero[1];
 
 // The wave's own LDS accesses are done, then all waves meet; what waves still
 // have in flight from global memory is left in flight.
-__device__ __forceinline__ void mm_barrier() {
+__device__ __forceinline__ void mm_wait_lds() {
+  asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0)
   asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void mm_barrier() {
+  mm_wait_lds();
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
@@ -419,14 +423,12 @@ __global__ __launch_bounds__(WR* WC* KG * 64, 2) void mm_kernel(MmArgs<T> a) {
   static_assert(NW * TJ * 16 * 64 * 4 <= NST * SU * 16, "64 rows of every wave");
 #pragma unroll
   for (int g = 0; g < TI / 4; ++g) {
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the wave's own accesses, in order
-    asm volatile("" ::: "memory");
+    mm_wait_lds();  // the wave's own accesses, in order
 #pragma unroll
     for (int j = 0; j < TJ; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) own[(16 * j + fr) * 16 + ((4 * i + q) ^ fr)] = acc[4 * g + i][j];
-    __builtin_amdgcn_s_waitcnt(0xC07F);  // lgkmcnt(0): the wave's own accesses, in order
-    asm volatile("" ::: "memory");
+    mm_wait_lds();  // the wave's own accesses, in order
     const long long r0w = r0 + xr + 64 * g;
     if (a.vec || a.splits > 1) {
       constexpr int N = 16 / sizeof(OT), L = 64 / N;  // outputs of a lane, lanes of a column
