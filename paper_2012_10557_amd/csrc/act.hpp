@@ -14,10 +14,21 @@ enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2, ACT_GELU = 3 };
 
 // 1 / (1 + exp(-u)); exp(-u) may overflow, the quotient is then 0.  bf16: the
 // hardware's exp2 and reciprocal, off by about (|u| + 2) 2^-24, far below the
-// 2^-9 of the result's rounding.
+// 2^-9 of the result's rounding.  fp32: the same two, the exponent in two parts
+// (what u log2 e loses is added to first order) and a Newton step on the
+// reciprocal, off by 3 halves of a step; library exponential and division took
+// 25 us where this takes 20 (group norm backward, 19 x 1147 x 120).
 template <typename T> __device__ __forceinline__ float sigmoid_of(float u) {
 #pragma clang fp contract(off)
-  if constexpr (sizeof(T) == 4) return 1.f / (1.f + expf(-u));
+  if constexpr (sizeof(T) == 4) {
+    const float t = u * -1.44269502f;
+    const float lo = fmaf(u, -1.44269502f, -t) + u * -1.92596299e-8f;
+    const bool in = t < 126.f;
+    float e = __builtin_amdgcn_exp2f(t);
+    e = in ? fmaf(e, 0.693147181f * lo, e) : e;
+    const float d = 1.f + e, r = __builtin_amdgcn_rcpf(d);
+    return in ? fmaf(fmaf(-d, r, 1.f), r, r) : r;
+  }
   return __builtin_amdgcn_rcpf(1.f + __expf(-u));
 }
 

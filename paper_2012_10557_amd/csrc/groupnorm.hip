@@ -73,6 +73,7 @@ struct GnArgs {
   float* part;                // [N][slots][C][2] (backward: [N][chunks][2][C])
   float* tot;                 // [N][2][C] (backward)
   float* coef;                // [N][G][2] (backward)
+  float* slices;              // [GN_SLICES][2][C] (backward)
   float *dgamma, *dbeta;
   long long HW;
   int N, C, G, gs;       // gs: channels of a group
@@ -334,61 +335,76 @@ __global__ __launch_bounds__(GN_NT) void gn_bwd_sums_kernel(GnArgs a) {
   }
 }
 
-// tot[n][2][c] = sums over the sample's chunks of part[n][chunk][2][c]: 32
-// columns a block, 32 threads a column.
-__global__ __launch_bounds__(1024) void gn_bwd_fold_kernel(GnArgs a) {
+// Sums of src's columns over `per` rows a slice: 32 columns a block, 32 threads
+// a column.  out: [slice][cols]; null: the sums are dbeta and dgamma.
+struct GnColumns {
+  const float* src;
+  long long rows, per;
+  int cols, blocks;  // blocks of a slice
+  float* out;
+};
+__device__ __forceinline__ void gn_columns(const GnArgs& a, const GnColumns& k, int b) {
   __shared__ float red[32][33];
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, per = (2 * a.C + 31) / 32;
-  const int n = blockIdx.x / per, c = (blockIdx.x - n * per) * 32 + x;
-  const float* p = a.part + (long long)n * a.chunks * 2 * a.C + c;
+  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, slice = b / k.blocks;
+  const int c = (b - slice * k.blocks) * 32 + x;
+  const long long r1 = min(k.rows, (slice + 1) * k.per);
   float s = 0.f;
-  if (c < 2 * a.C)
-#pragma unroll 4
-    for (int k = y; k < a.chunks; k += 32) s += p[(long long)k * 2 * a.C];
-  red[y][x] = s;
-  __syncthreads();
-  for (int h = 16; h > 0; h >>= 1) {
-    if (y < h) red[y][x] += red[y + h][x];
-    __syncthreads();
-  }
-  if (y == 0 && c < 2 * a.C) a.tot[(long long)n * 2 * a.C + c] = red[0][x];
-}
-
-// coef = (avg h, avg h * xhat) of a (sample, group): a block each.
-__global__ __launch_bounds__(GN_NT) void gn_bwd_coef_kernel(GnArgs a) {
-  __shared__ float red[4];
-  const int t = threadIdx.x, n = blockIdx.x / a.G, g = blockIdx.x - n * a.G;
-  const float* tot = a.tot + (long long)n * 2 * a.C + g * a.gs;
-  float s = 0.f, q = 0.f;
-  for (int c = t; c < a.gs; c += GN_NT) {
-    const float w = a.gamma ? a.gamma[g * a.gs + c] : 1.f;
-    s += w * tot[c];
-    q += w * tot[a.C + c];
-  }
-  s = block_sum(s, red);
-  q = block_sum(q, red);
-  const float inv = 1.f / ((float)a.HW * a.gs);
-  if (t == 0) {
-    a.coef[2 * (long long)blockIdx.x] = s * inv;
-    a.coef[2 * (long long)blockIdx.x + 1] = q * inv;
-  }
-}
-
-// dbeta and dgamma: tot summed over the samples.
-__global__ __launch_bounds__(1024) void gn_bwd_param_kernel(GnArgs a) {
-  __shared__ float red[32][33];
-  const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
-  float s = 0.f;
-  if (c < 2 * a.C)
+  if (c < k.cols)
 #pragma unroll 8
-    for (int n = y; n < a.N; n += 32) s += a.tot[(long long)n * 2 * a.C + c];
+    for (long long r = slice * k.per + y; r < r1; r += 32) s += k.src[r * k.cols + c];
   red[y][x] = s;
   __syncthreads();
   for (int h = 16; h > 0; h >>= 1) {
     if (y < h) red[y][x] += red[y + h][x];
     __syncthreads();
   }
-  if (y == 0 && c < 2 * a.C) (c < a.C ? a.dbeta + c : a.dgamma + (c - a.C))[0] = red[0][x];
+  if (y == 0 && c < k.cols) {
+    if (k.out)
+      k.out[(long long)slice * k.cols + c] = red[0][x];
+    else
+      (c < a.C ? a.dbeta + c : a.dgamma + (c - a.C))[0] = red[0][x];
+  }
+}
+__global__ __launch_bounds__(1024) void gn_columns_kernel(GnArgs a, GnColumns k) { gn_columns(a, k, blockIdx.x); }
+
+// Blocks from `first` on: coef = (avg h, avg h * xhat) of 4 (sample, group)s,
+// 256 threads each, from the chunks' partial sums; those before: column sums.
+__global__ __launch_bounds__(1024) void gn_bwd_coef_kernel(GnArgs a, GnColumns k, int first) {
+  __shared__ float red[2][16];
+  if ((int)blockIdx.x < first) {
+    gn_columns(a, k, blockIdx.x);
+    return;
+  }
+  const int t = threadIdx.x & 255, w = threadIdx.x >> 6;
+  const long long i = ((long long)blockIdx.x - first) * 4 + (threadIdx.x >> 8);
+  const int n = (int)(i / a.G), g = (int)(i - (long long)n * a.G);
+  float s = 0.f, q = 0.f;
+  if (n < a.N) {
+    const float* part = a.part + (long long)n * a.chunks * 2 * a.C + g * a.gs;
+    const int count = a.chunks * a.gs;
+    for (int j = t; j < count; j += 256) {
+      const int r = j / a.gs, c = j - r * a.gs;
+      const float* p = part + (long long)r * 2 * a.C + c;
+      const float m = a.gamma ? a.gamma[g * a.gs + c] : 1.f;
+      s += m * p[0];
+      q += m * p[a.C];
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    s += __shfl_xor(s, o, 64);
+    q += __shfl_xor(q, o, 64);
+  }
+  if ((threadIdx.x & 63) == 0) {
+    red[0][w] = s;
+    red[1][w] = q;
+  }
+  __syncthreads();
+  if (t == 0 && n < a.N) {
+    const float inv = 1.f / ((float)a.HW * a.gs);
+    a.coef[2 * i] = ((red[0][w] + red[0][w + 1]) + (red[0][w + 2] + red[0][w + 3])) * inv;
+    a.coef[2 * i + 1] = ((red[1][w] + red[1][w + 1]) + (red[1][w + 2] + red[1][w + 3])) * inv;
+  }
 }
 
 template <typename T, int E, int ACT>
@@ -699,7 +715,7 @@ template <typename F> hipError_t gn_samples(GnArgs a, size_t esize, long long pe
     b.out = (char*)a.out + off;
     b.mean = a.mean + n * a.G;
     b.rstd = a.rstd + n * a.G;
-    b.part = a.part + n * std::max(a.chunks, a.slots) * 2 * a.C;
+    b.part = a.part + n * (a.dy ? a.chunks : a.slots) * 2 * a.C;
     if (a.tot) b.tot = a.tot + n * 2 * a.C;
     if (a.coef) b.coef = a.coef + n * 2 * a.G;
     EKYA_HIP(go(b, dim3((unsigned)(b.N * per))));
@@ -779,6 +795,21 @@ template <typename T, int E> hipError_t gn_forward(GnArgs a, int act, hipStream_
   });
 }
 
+// dbeta and dgamma as the column sums of src [rows][2 C]; more than GN_ROWS rows
+// are first added up in slices, into a.slices.
+constexpr long long GN_ROWS = 4096;
+constexpr int GN_SLICES = 128;
+hipError_t gn_param(const GnArgs& a, const float* src, long long rows, GnColumns& k, hipStream_t st) {
+  k = {src, rows, std::max(1LL, rows), 2 * a.C, cdiv(2 * a.C, 32), nullptr};
+  if (rows <= GN_ROWS) return hipSuccess;
+  k.per = cdivl(rows, GN_SLICES);
+  k.out = a.slices;
+  const long long slices = cdivl(rows, k.per);
+  hipLaunchKernelGGL(gn_columns_kernel, dim3((unsigned)(slices * k.blocks)), dim3(1024), 0, st, a, k);
+  k = {a.slices, slices, slices, k.cols, k.blocks, nullptr};
+  return hipGetLastError();
+}
+
 template <typename T, int E> hipError_t gn_backward(GnArgs a, int act, hipStream_t st) {
   if constexpr (E > 1) {
     // 8-byte units in bf16: a unit's constants and sums take half the registers
@@ -795,11 +826,11 @@ template <typename T, int E> hipError_t gn_backward(GnArgs a, int act, hipStream
           return hipGetLastError();
         });
       })));
-      if (a.dgamma) {
-        hipLaunchKernelGGL(gn_bwd_param_kernel, dim3(cdiv(2 * a.C, 32)), dim3(1024), 0, st, a);
-        EKYA_HIP(hipGetLastError());
-      }
-      return hipSuccess;
+      if (!a.dgamma) return hipSuccess;
+      GnColumns k;
+      EKYA_HIP(gn_param(a, a.tot, a.N, k, st));
+      hipLaunchKernelGGL(gn_columns_kernel, dim3(k.blocks), dim3(1024), 0, st, a, k);
+      return hipGetLastError();
     }
   }
   gn_cut(a, E);
@@ -810,18 +841,19 @@ template <typename T, int E> hipError_t gn_backward(GnArgs a, int act, hipStream
       return hipGetLastError();
     });
   }));
-  EKYA_HIP(gn_samples(a, sizeof(T), cdiv(2 * a.C, 32), [&](const GnArgs& b, dim3 grid) {
-    hipLaunchKernelGGL(gn_bwd_fold_kernel, grid, dim3(1024), 0, st, b);
-    return hipGetLastError();
-  }));
-  EKYA_HIP(gn_samples(a, sizeof(T), a.G, [&](const GnArgs& b, dim3 grid) {
-    hipLaunchKernelGGL(gn_bwd_coef_kernel, grid, dim3(GN_NT), 0, st, b);
-    return hipGetLastError();
-  }));
-  if (a.dgamma) {
-    hipLaunchKernelGGL(gn_bwd_param_kernel, dim3(cdiv(2 * a.C, 32)), dim3(1024), 0, st, a);
+  GnColumns k{};
+  if (a.dgamma) EKYA_HIP(gn_param(a, a.part, (long long)a.N * a.chunks, k, st));
+  int first = k.blocks;  // the first launch takes the parameters' sums with it
+  if (a.N == 0 && first) {
+    hipLaunchKernelGGL(gn_columns_kernel, dim3(first), dim3(1024), 0, st, a, k);
     EKYA_HIP(hipGetLastError());
   }
+  EKYA_HIP(gn_samples(a, sizeof(T), a.G, [&](const GnArgs& b, dim3) {
+    hipLaunchKernelGGL(gn_bwd_coef_kernel, dim3((unsigned)(first + cdivl((long long)b.N * b.G, 4))), dim3(1024), 0,
+                       st, b, k, first);
+    first = 0;
+    return hipGetLastError();
+  }));
   return gn_samples(a, sizeof(T), per, [&](const GnArgs& b, dim3 grid) {
     return act_dispatch(act, [&](auto k) {
       hipLaunchKernelGGL((gn_bwd_apply_kernel<T, E, k.value>), grid, dim3(GN_NT), 0, st, b);
@@ -853,7 +885,7 @@ size_t groupnorm_workspace_floats(int dt, int N, long long HW, int C, int G, boo
   const int E = dtype_vec(dt);
   size_t f = gn_part_floats(a, 1);
   if (C % E == 0) f = std::max(f, gn_part_floats(a, E));
-  if (backward) f += (size_t)N * 2 * (C + (size_t)G);
+  if (backward) f += (size_t)N * 2 * (C + (size_t)G) + (size_t)GN_SLICES * 2 * C;
   return f;
 }
 
@@ -891,7 +923,8 @@ hipError_t groupnorm_bwd(int dt, const void* dy, const void* x, int N, long long
   a.dbeta = dbeta;
   a.tot = ws;
   a.coef = a.tot + (size_t)N * 2 * C;
-  a.part = a.coef + (size_t)N * 2 * G;
+  a.slices = a.coef + (size_t)N * 2 * G;
+  a.part = a.slices + (size_t)GN_SLICES * 2 * C;
   const bool unit = C % dtype_vec(dt) == 0 && unit_ok(x) && unit_ok(dy) && unit_ok(dx);
   if (dt == DT_BF16)
     return unit ? gn_backward<bf16, 8>(a, act, st) : gn_backward<bf16, 1>(a, act, st);

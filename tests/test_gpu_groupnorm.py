@@ -233,3 +233,14 @@ def test_groupnorm_on_a_stream_and_in_a_graph():
         torch.cuda.synchronize()
         assert torch.equal(y, ey) and torch.equal(mean, em) and torch.equal(rstd, er), i
         assert all(torch.equal(a, b) for a, b in zip(grads, eg)), i
+
+
+@pytest.mark.parametrize("N,HW,C,G", [(6000, 4, 16, 4), (5000, 3, 6, 2)])
+def test_parameter_gradients_of_many_samples(N, HW, C, G):
+    """More samples than one pass over their sums takes."""
+    import torch
+    x, dy, gamma, beta = _inputs(N, HW, C, torch.bfloat16)
+    y, mean, rstd = _forward(x, G, gamma, beta, "relu")
+    check_forward(x, G, gamma, beta, "relu", y, mean, rstd)
+    dx, dgamma, dbeta = _backward(dy, x, G, gamma, beta, mean, rstd, "relu")
+    check_backward(dy, x, G, gamma, beta, mean, rstd, "relu", dx, dgamma, dbeta)
