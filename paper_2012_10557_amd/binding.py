@@ -10,6 +10,7 @@ this module without it raises an error.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 from typing import List, Optional, Sequence
 
@@ -246,6 +247,7 @@ def _check(status: int, ctx=None):
 
 
 # -------------------------------------------------------------- tensors
+@functools.lru_cache(maxsize=None)
 def _torch():
     import torch
     return torch
@@ -751,8 +753,8 @@ def _raw_stream(device: int) -> int:
     return _torch()._C._cuda_getCurrentRawStream(device)
 
 
-def _scratch(nbytes: int, device):
-    return _torch().empty(nbytes, dtype=_torch().uint8, device=device) if nbytes else None
+def _scratch(nbytes: int, like):
+    return like.new_empty(nbytes, dtype=_torch().uint8) if nbytes else None
 
 
 def _ptr(t, shape, dtype, name: str):
@@ -771,11 +773,18 @@ def _ptr(t, shape, dtype, name: str):
 def _groupnorm_dims(x):
     if x.dim() < 2:
         raise ValueError("group norm needs [N, ..., C]")
-    N, *mid, C = x.shape
+    shape = x.shape
     hw = 1
-    for n in mid:
+    for n in shape[1:-1]:
         hw *= n
-    return N, hw, C
+    return shape[0], hw, shape[-1]
+
+
+@functools.lru_cache(maxsize=256)
+def _groupnorm_workspace(backward: bool, prec: int, N: int, HW: int, C: int, groups: int) -> int:
+    lib = load()
+    query = lib.ekya_op_groupnorm_backward_workspace if backward else lib.ekya_op_groupnorm_workspace
+    return query(prec, N, HW, C, groups)
 
 
 def ekya_op_groupnorm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5,
@@ -785,12 +794,11 @@ def ekya_op_groupnorm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5,
     lib = load()
     N, HW, C = _groupnorm_dims(x)
     d = _on_current(x, gamma, beta, y)
-    prec, dt, f32, dev, shape = _precision(x), x.dtype, torch.float32, x.device, x.shape
-    y = torch.empty(shape, dtype=dt, device=dev) if y is None else y
-    mean = torch.empty((N, max(groups, 0)), dtype=f32, device=dev)
-    rstd = torch.empty((N, max(groups, 0)), dtype=f32, device=dev)
-    nbytes = lib.ekya_op_groupnorm_workspace(prec, N, HW, C, groups)
-    ws = _scratch(nbytes, dev)
+    prec, dt, f32, shape = _precision(x), x.dtype, torch.float32, x.shape
+    y = x.new_empty(shape) if y is None else y
+    mean, rstd = x.new_empty((2, N, max(groups, 0)), dtype=f32).unbind(0)
+    nbytes = _groupnorm_workspace(False, prec, N, HW, C, groups)
+    ws = _scratch(nbytes, x)
     _op(lib.ekya_op_groupnorm(prec, _ptr(x, shape, dt, "x"), N, HW, C, groups,
                               _ptr(gamma, (C,), f32, "gamma"), _ptr(beta, (C,), f32, "beta"), eps, act,
                               _ptr(y, shape, dt, "y"), mean.data_ptr(), rstd.data_ptr(),
@@ -805,12 +813,11 @@ def ekya_op_groupnorm_backward(dy, x, groups: int, gamma, beta, mean, rstd,
     lib = load()
     N, HW, C = _groupnorm_dims(x)
     d = _on_current(x, dy, gamma, beta, mean, rstd, dx)
-    prec, dt, f32, dev, shape = _precision(x), x.dtype, torch.float32, x.device, x.shape
-    dx = torch.empty(shape, dtype=dt, device=dev) if dx is None else dx
-    dgamma = torch.empty(C, dtype=f32, device=dev)
-    dbeta = torch.empty(C, dtype=f32, device=dev)
-    nbytes = lib.ekya_op_groupnorm_backward_workspace(prec, N, HW, C, groups)
-    ws = _scratch(nbytes, dev)
+    prec, dt, f32, shape = _precision(x), x.dtype, torch.float32, x.shape
+    dx = x.new_empty(shape) if dx is None else dx
+    dgamma, dbeta = x.new_empty((2, C), dtype=f32).unbind(0)
+    nbytes = _groupnorm_workspace(True, prec, N, HW, C, groups)
+    ws = _scratch(nbytes, x)
     _op(lib.ekya_op_groupnorm_backward(
         prec, _ptr(dy, shape, dt, "dy"), _ptr(x, shape, dt, "x"), N, HW, C, groups,
         _ptr(gamma, (C,), f32, "gamma"), _ptr(beta, (C,), f32, "beta"),
@@ -850,15 +857,15 @@ def ekya_op_matmul(x, w, bias=None, act: int = EKYA_ACT_NONE, residual=None,
     lib = load()
     M, N, K = _matmul_dims(x, w)
     d = _on_current(x, w, bias, residual, y)
-    dt, dev = x.dtype, x.device
-    y = torch.empty((M, N), dtype=dt, device=dev) if y is None else y
-    z = torch.empty((M, N), dtype=dt, device=dev) if keep_z else None
+    dt = x.dtype
+    y = x.new_empty((M, N)) if y is None else y
+    z = x.new_empty((M, N)) if keep_z else None
     a = MatmulArgs(_precision(x), M, N, K, *_matrix(x, M, K, dt, "x"), *_matrix(w, N, K, dt, "w"),
                    _ptr(bias, (N,), torch.float32, "bias"), act, *_matrix(residual, M, N, dt, "residual"),
                    residual_first, *_matrix(y, M, N, dt, "y"), *_matrix(z, M, N, dt, "z"))
     args = ctypes.byref(a)
     nbytes = lib.ekya_op_matmul_workspace(args)
-    ws = _scratch(nbytes, dev)
+    ws = _scratch(nbytes, x)
     _op(lib.ekya_op_matmul(args, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(d)))
     return y, z
 
@@ -873,7 +880,7 @@ def ekya_op_matmul_backward(dy, x, w, act: int = EKYA_ACT_NONE, z=None, dw_dtype
     lib = load()
     M, N, K = _matmul_dims(x, w)
     d = _on_current(x, w, dy, z, dx, dz)
-    dt, dev, f32 = x.dtype, x.device, torch.float32
+    dt, f32 = x.dtype, torch.float32
     dw_dtype = f32 if dw_dtype is None else dw_dtype
     if dw_dtype not in (f32, dt):
         raise TypeError(f"dw: expected float32 or {dt}, got {dw_dtype}")
@@ -882,13 +889,13 @@ def ekya_op_matmul_backward(dy, x, w, act: int = EKYA_ACT_NONE, z=None, dw_dtype
     elif z is None:
         raise ValueError("z is needed behind an activation")
     elif dz is None:
-        dz = torch.empty((M, N), dtype=dt, device=dev)
+        dz = x.new_empty((M, N))
     if not need_dx:
         dx = None
     elif dx is None:
-        dx = torch.empty((M, K), dtype=dt, device=dev)
-    dw = torch.empty((N, K), dtype=dw_dtype, device=dev) if need_dw else None
-    db = torch.empty(N, dtype=f32, device=dev) if need_db else None
+        dx = x.new_empty((M, K))
+    dw = x.new_empty((N, K), dtype=dw_dtype) if need_dw else None
+    db = x.new_empty(N, dtype=f32) if need_db else None
     a = MatmulBackwardArgs(_precision(x), M, N, K, *_matrix(dy, M, N, dt, "dy"),
                            *_matrix(z, M, N, dt, "z"), act, *_matrix(x, M, K, dt, "x"),
                            *_matrix(w, N, K, dt, "w"), *_matrix(dz, M, N, dt, "dz"),
@@ -896,7 +903,7 @@ def ekya_op_matmul_backward(dy, x, w, act: int = EKYA_ACT_NONE, z=None, dw_dtype
                            EKYA_FP32 if dw_dtype == f32 else EKYA_BF16, db.data_ptr() if need_db else None)
     args = ctypes.byref(a)
     nbytes = lib.ekya_op_matmul_backward_workspace(args)
-    ws = _scratch(nbytes, dev)
+    ws = _scratch(nbytes, x)
     _op(lib.ekya_op_matmul_backward(args, ws.data_ptr() if nbytes else None, nbytes, _raw_stream(d)))
     return dx, dw, db, dz
 
