@@ -6,6 +6,13 @@
 // operation (no fused multiply-add), so that the states, and with 8 bits the
 // codes that their rounding picks, do not depend on how a compiler contracts
 // it.
+//
+// Bound by HBM: 32-bit states with fp32 gradients and a bf16 copy move 30 bytes
+// a weight (the ResNet18's 62 tensors, 11.2 M weights: 67 us, 5.0 TB/s), 8-bit
+// states with bf16 gradients and the copy 16 (134 M weights: 396 us, 5.4 TB/s); a
+// large copy reaches 5.1 TB/s.  Two small tensors take 4 us.  Blocks of 256 share
+// a scale so that a wave finds their largest value without LDS, and four
+// elements a lane make one 16-byte access of the fp32 arrays.
 #include <algorithm>
 #include <cmath>
 
