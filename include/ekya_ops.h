@@ -109,7 +109,8 @@ ekya_status ekya_op_resize(int precision, const void* frames, int n, int H, int 
  * device), allocate nothing, copy nothing and never wait, so they can be
  * captured into a HIP graph.  Scratch memory is the caller's: `workspace`, at
  * least as many bytes as the matching *_workspace query says (host only, 0 if
- * an argument is invalid), on 16 bytes, written before it is read, free for
+ * an argument is invalid; a query that takes the call's arguments looks at their
+ * addresses too), on 16 bytes, written before it is read, free for
  * other use once the call's work has run; calls that may overlap on the GPU,
  * and graphs that may, need one each.  Types per `precision` as above; any
  * channel count, size and alignment to the element is accepted.  Results do

@@ -915,11 +915,12 @@ class Adamw:
     def __init__(self, handle, tensors, grads):
         self.handle, self.tensors, self.grads = handle, tensors, grads
         self.device = grads[0].device if grads else None
+        self._destroy = load().ekya_adamw_destroy
 
     def close(self) -> None:
         handle, self.handle = self.handle, None
         if handle:
-            load().ekya_adamw_destroy(handle)
+            self._destroy(handle)
 
     __del__ = close
 

@@ -42,13 +42,12 @@ template <typename T> __device__ __forceinline__ float normal_cdf(float u, float
     e = expf(-0.5f * u * u);
     return 0.5f * erfcf(-0.70710678f * u);
   }
-  e = __expf(-0.5f * u * u);
+  e = __builtin_amdgcn_exp2f(u * u * -0.721347520f);
   const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f * 0.70710678f, fabsf(u), 1.f));
-  float p = fmaf(t, 1.061405429f, -1.453152027f);
-  p = fmaf(t, p, 1.421413741f);
-  p = fmaf(t, p, -0.284496736f);
-  p = t * fmaf(t, p, 0.254829592f);
-  const float h = 0.5f * p * e;
+  float p = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);  // half of it
+  p = fmaf(t, p, 0.5f * 1.421413741f);
+  p = fmaf(t, p, 0.5f * -0.284496736f);
+  const float h = t * fmaf(t, p, 0.5f * 0.254829592f) * e;
   return u < 0.f ? h : 1.f - h;
 }
 
