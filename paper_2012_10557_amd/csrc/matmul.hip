@@ -542,8 +542,25 @@ struct MmPlan {
 // 27.4 and 28.0.  256 against 512 blocks: 128 x 2048 x 8192 (parts of 32 and 16
 // stages) 12.6 and 15.7, 256 x 1024 x 25088 (98 and 49) 40.6 and 33.4.  A part has
 // 16 stages at least (1024 x 512 x 4096 in parts of 32, 16 and 8: 21.6, 17.5 and
-// 19.2), 6 in fp32 and 4 without DMA, whose stages take longer (1001 x 513 x 771
-// fp32 in two parts 22.1 us, in one 23.6).
+// 19.2), 4 without DMA, whose stages take longer.
+//
+// fp32 is bound by the matrix cores with two blocks a CU already, so its parts
+// are those whose rounds come out even: a stage takes 1.0 us where a CU has one
+// block and 0.6 for each where it has more, adding up 4 us and the partial
+// sums' traffic (212 x 5079 x 2955, 188 tiles: 106 us in two parts, 88 in four).
+int mm_fp32_parts(long long tiles, long long ns, double outputs) {
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= 16 && s <= std::max(1LL, ns / 4); ++s) {
+    const long long blocks = cdivl(tiles * s, 256);
+    const double us = cdivl(ns, s) * (blocks == 1 ? 1.0 : 0.6 * blocks) + (s > 1 ? 4 + s * outputs * 8 / 4e6 : 0);
+    if (us < least) {
+      least = us;
+      best = s;
+    }
+  }
+  return best;
+}
 MmPlan mm_plan(long long R, long long C, long long Tn, int dt, bool dma) {
   const long long ns = std::max(1LL, cdivl(Tn, 8 * dtype_vec(dt)));
   const long long t256 = cdivl(R, 256) * cdivl(C, 256), t128 = cdivl(R, 128) * cdivl(C, 128);
@@ -556,9 +573,9 @@ MmPlan mm_plan(long long R, long long C, long long Tn, int dt, bool dma) {
   }
   if (t128 >= 192) return {128, 1, (int)ns, 1};
   const long long t64 = std::max(1LL, cdivl(R, 64) * cdivl(C, 64));
-  const bool slow = !dma || dt != DT_BF16;
-  const long long blocks = slow || ns * t64 >= 512 * 32 ? 512 : 256;
-  const long long want = std::max(1LL, std::min(blocks / t64, ns / (!dma ? 4 : slow ? 6 : 16)));
+  const long long blocks = !dma || ns * t64 >= 512 * 32 ? 512 : 256;
+  const long long want = dt == DT_F32 ? mm_fp32_parts(t64, ns, (double)R * C)
+                                      : std::max(1LL, std::min(blocks / t64, ns / (dma ? 16 : 4)));
   const int stages = (int)cdivl(ns, want);
   return {64, (int)cdivl(ns, stages), stages, 1};
 }
