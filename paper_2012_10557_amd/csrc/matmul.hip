@@ -544,38 +544,42 @@ struct MmPlan {
 // 16 stages at least (1024 x 512 x 4096 in parts of 32, 16 and 8: 21.6, 17.5 and
 // 19.2), 4 without DMA, whose stages take longer.
 //
-// fp32 is bound by the matrix cores with two blocks a CU already, so its parts
-// are those whose rounds come out even: a stage takes 1.0 us where a CU has one
-// block and 0.6 for each where it has more, adding up 4 us and the partial
-// sums' traffic (212 x 5079 x 2955, 188 tiles: 106 us in two parts, 88 in four).
-int mm_fp32_parts(long long tiles, long long ns, double outputs) {
-  int best = 1;
+// fp32 is bound by the matrix cores with a block or two a CU already, so tile and
+// parts are those whose rounds come out even: a stage of a 128 x 128 tile takes
+// 2.3 us where a CU has one block and 2.0 for each where it has more, of 64 x 64
+// 1.0 and 0.6; adding up takes 4 us and the partial sums' traffic.  212 x 5079 x
+// 2955: 64 x 64 in two parts (188 tiles) 114 us, in four 94; 16384 x 512 x 300 dx:
+// 384 tiles of 128 72 us, 1280 of 64 54.
+MmPlan mm_fp32_plan(long long R, long long C, long long ns) {
+  MmPlan best{};
   double least = 1e30;
-  for (int s = 1; s <= 16 && s <= std::max(1LL, ns / 4); ++s) {
-    const long long blocks = cdivl(tiles * s, 256);
-    const double us = cdivl(ns, s) * (blocks == 1 ? 1.0 : 0.6 * blocks) + (s > 1 ? 4 + s * outputs * 8 / 4e6 : 0);
-    if (us < least) {
-      least = us;
-      best = s;
+  for (int tile : {64, 128})
+    for (int s = 1; s <= 16 && s <= std::max(1LL, ns / 4); ++s) {
+      const long long stages = cdivl(ns, s), blocks = cdivl(cdivl(R, tile) * cdivl(C, tile) * s, 256);
+      const double stage = tile == 128 ? (blocks == 1 ? 2.3 : 2.0 * blocks) : blocks == 1 ? 1.0 : 0.6 * blocks;
+      const double us = stages * stage + (s > 1 ? 4 + s * (double)R * C * 8 / 4e6 : 0);
+      if (us < least) {
+        least = us;
+        best = {tile, (int)cdivl(ns, stages), (int)stages, 1};
+      }
     }
-  }
   return best;
 }
 MmPlan mm_plan(long long R, long long C, long long Tn, int dt, bool dma) {
   const long long ns = std::max(1LL, cdivl(Tn, 8 * dtype_vec(dt)));
   const long long t256 = cdivl(R, 256) * cdivl(C, 256), t128 = cdivl(R, 128) * cdivl(C, 128);
-  if (dma && dt == DT_BF16 && t256 >= 192 &&
+  if (dt == DT_F32) return mm_fp32_plan(R, C, ns);
+  if (dma && t256 >= 192 &&
       cdivl(t256, 256) * (10 + 1.58 * ns) <= 5 + t128 / 256. * (2.3 + 0.46 * ns))
     return {256, 1, (int)ns, 1};
-  if (dma && dt == DT_BF16 && std::min(R, C) >= 128 && t128 <= 256 && ns * t128 >= 512 * 8) {
+  if (dma && std::min(R, C) >= 128 && t128 <= 256 && ns * t128 >= 512 * 8) {
     const long long parts = 2 * (256 / t128), stages = cdivl(ns, parts);
     return {128, (int)cdivl(ns, 2 * stages), (int)stages, 2};
   }
   if (t128 >= 192) return {128, 1, (int)ns, 1};
   const long long t64 = std::max(1LL, cdivl(R, 64) * cdivl(C, 64));
   const long long blocks = !dma || ns * t64 >= 512 * 32 ? 512 : 256;
-  const long long want = dt == DT_F32 ? mm_fp32_parts(t64, ns, (double)R * C)
-                                      : std::max(1LL, std::min(blocks / t64, ns / (dma ? 16 : 4)));
+  const long long want = std::max(1LL, std::min(blocks / t64, ns / (dma ? 16 : 4)));
   const int stages = (int)cdivl(ns, want);
   return {64, (int)cdivl(ns, stages), stages, 1};
 }
