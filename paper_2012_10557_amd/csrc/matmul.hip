@@ -10,7 +10,7 @@
 // r is the direction in which the result lies in memory, t the reduction; an
 // operand marked ^ lies in memory with t as its rows.  A block of 4 or 8 waves
 // owns a tile of D; stages of 128 bytes of the reduction per row (64 bf16, 32
-// fp32: whole cache lines) pass through two buffers in LDS, and the fragments
+// fp32: whole cache lines) pass through two or three buffers in LDS, and the fragments
 // of the next half stage are read into registers while the matrix cores work on
 // this one's.
 //
@@ -534,6 +534,13 @@ struct MmPlan {
 // for.  Measured, 256 against 128: 8192^3 826 and 962 us, 4096^3 114 and 123,
 // 6272 x 2048 x 512 (200 tiles of 256) 23.2 and 25.2, 25088 x 1024 x 256 30.4 and
 // 31.1, 2048^3 (64 tiles of 256) 53.6 and 27.4.
+//
+// Up to 256 tiles of 128 with a reduction long enough for 512 parts of 8 stages:
+// two groups of waves a block, each with a part of the reduction, which overlap as
+// two blocks would and leave half the partial sums.  One group or 64 x 64 against
+// two groups: 2048^3 27.0 and 24.7 us, dw of 6272 x 512 x 2048 31.5 and 28.0, of
+// 25088 x 256 x 1024 30.7 and 27.1; 1500 x 4000 x 1500, whose 144 tiles leave CUs
+// idle, loses: 46.0 and 48.6.
 //
 // With less than 192 tiles of 128 most CUs hold one block or none: 64 x 64, and
 // the reduction split until 512 blocks run where a part is still 32 stages
