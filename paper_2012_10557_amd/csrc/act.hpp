@@ -17,13 +17,16 @@ enum Act { ACT_NONE = 0, ACT_RELU = 1, ACT_SILU = 2, ACT_GELU = 3 };
 // 2^-9 of the result's rounding.  fp32: the same two, the exponent in two parts
 // (what u log2 e loses is added to first order) and a Newton step on the
 // reciprocal, off by 3 halves of a step; library exponential and division took
-// 25 us where this takes 20 (group norm backward, 19 x 1147 x 120).
+// 25 us where this takes 20 (group norm backward, 19 x 1147 x 120).  From
+// |u| = 87.3 on neither the second part nor the step is taken: exp(-u) is then
+// below 2^-126 and the quotient 1, or the quotient below 2^-126 and 0, and parts
+// of an infinite exponent would make it NaN.
 template <typename T> __device__ __forceinline__ float sigmoid_of(float u) {
 #pragma clang fp contract(off)
   if constexpr (sizeof(T) == 4) {
     const float t = u * -1.44269502f;
     const float lo = fmaf(u, -1.44269502f, -t) + u * -1.92596299e-8f;
-    const bool in = t < 126.f;
+    const bool in = fabsf(t) < 126.f;
     float e = __builtin_amdgcn_exp2f(t);
     e = in ? fmaf(e, 0.693147181f * lo, e) : e;
     const float d = 1.f + e, r = __builtin_amdgcn_rcpf(d);
