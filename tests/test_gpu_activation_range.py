@@ -8,7 +8,7 @@ import pytest
 from tests.adapter_ref import ACTS, U, act64, half_step
 
 pytestmark = pytest.mark.gpu
-SILU = 2
+SILU, GELU = 2, 3
 BEYOND = [100.0, 1e30, 2.3e38, 2.5e38, 3e38, float("inf")]
 
 
@@ -97,3 +97,29 @@ def test_the_other_activations_of_large_values():
             assert torch.equal(y, u if act == "none" else u.clamp(min=0)), act
             fin = torch.isfinite(u)  # u phi(u) of inf is not a number
             assert act == "none" or torch.equal(slope[fin], (u > 0).to(dtype)[fin]), act
+
+
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+def test_gelu_keeps_its_digits_far_below_zero(prec):
+    """The normal distribution's lower tail P is off by r P.  fp32: erfc of an argument off by 3 U,
+    which its tail takes u^2 times, and 64 U of the function's own.  bf16: the fit's 1.04e-4 (a 37th of
+    half a step), an exponential whose argument u^2 / 2 is off by 2 U of itself, and 32 U of the
+    polynomial and its constants.  Above 0 the result is 1 - P.  The slope P + u phi adds the error
+    of phi, the same as the exponential's; three roundings each."""
+    import math
+    import torch
+    dtype = torch.float32 if prec == "f32" else torch.bfloat16
+    u = torch.linspace(-13, 13, 6657, dtype=torch.float64).cuda().to(dtype)
+    y, slope = _apply(u, GELU)
+    u64, size = u.double(), u.double().abs()
+    exponential = (2 * size * size + 8) * U
+    rel = (4 * size * size + 64) * U if prec == "f32" else 1.04e-4 + exponential + 32 * U
+    tail = 0.5 * torch.special.erfc(size / math.sqrt(2))
+    P, dens = 0.5 * torch.special.erfc(-u64 / math.sqrt(2)), torch.exp(-0.5 * u64 * u64) / math.sqrt(2 * math.pi)
+    dP = rel * tail + 2 * U * P
+    half = half_step(dtype)
+    for got, ref, err in ((y, u64 * P, size * (dP + U * P)),
+                          (slope, P + u64 * dens, dP + size * dens * (exponential + 3 * U) + 2 * U * (P + size * dens))):
+        bound = 1.01 * err + half * (ref.abs() + 1.01 * err) + 2.0 ** -126 * 14
+        ok = (got.double() - ref).abs() <= bound
+        assert ok.all(), [(float(a), float(g), float(r)) for a, g, r in zip(u64[~ok], got[~ok], ref[~ok])][:8]
