@@ -127,9 +127,9 @@ typedef enum {
  * normalised by its own mean and biased variance over HW * C / groups
  * elements: u = (x - mean) * rstd * gamma + beta, rstd = 1 / sqrt(var + eps),
  * y = act(u).  gamma and beta [C] fp32, both or neither (null: 1 and 0).
- * mean, rstd: [N, groups] fp32 outputs, read by the backward pass.  y may be x
- * and overlaps it in no other way.  N >= 0 (0: nothing is done), HW >= 1, C in
- * [1, 65536], N * HW * C <= 2^40, eps > 0. */
+ * mean, rstd: [N, groups] fp32 outputs, read by the backward pass.  y may be x;
+ * otherwise no output overlaps an input or another output.  N >= 0 (0: nothing
+ * is done), HW >= 1, C in [1, 65536], N * HW * C <= 2^40, eps > 0. */
 size_t ekya_op_groupnorm_workspace(int precision, int N, long long HW, int C, int groups);
 ekya_status ekya_op_groupnorm(int precision, const void* x, int N, long long HW, int C, int groups,
                               const float* gamma, const float* beta, float eps, int act, void* y,
@@ -138,9 +138,9 @@ ekya_status ekya_op_groupnorm(int precision, const void* x, int N, long long HW,
 /* Its gradient: with g = dy * act'(u), dbeta = sum g and dgamma = sum g * xhat
  * over samples and pixels, h = g * gamma and dx = rstd * (h - avg(h) -
  * xhat * avg(h * xhat)), averages over the (sample, group).  dgamma and dbeta
- * [C] fp32, both or neither; N = 0 makes them zero.  dx may be dy or x, and
- * overlaps them in no other way.  gamma, beta, mean and rstd as the forward
- * call had and returned them. */
+ * [C] fp32, both or neither; N = 0 makes them zero.  dx may be dy or x;
+ * otherwise no output overlaps an input or another output.  gamma, beta, mean and
+ * rstd as the forward call had and returned them. */
 size_t ekya_op_groupnorm_backward_workspace(int precision, int N, long long HW, int C, int groups);
 ekya_status ekya_op_groupnorm_backward(int precision, const void* dy, const void* x, int N,
                                        long long HW, int C, int groups, const float* gamma,

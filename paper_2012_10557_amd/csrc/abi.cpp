@@ -699,7 +699,23 @@ bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return a && b && x < y + nb && y < x + na;
 }
-bool partial_overlap(const void* a, const void* b, size_t n) { return a != b && overlap(a, n, b, n); }
+
+// A range of bytes; none where it is null or empty.
+struct Span {
+  const void* p;
+  size_t n;
+  bool in_place;  // of an input: an output of the same range may take its place
+};
+// Whether an output shares a byte with an input or another output.
+bool outputs_overlap(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  for (const Span& o : outs) {
+    for (const Span& i : ins)
+      if (o.n && i.n && overlap(o.p, o.n, i.p, i.n) && !(o.in_place && i.in_place && o.p == i.p)) return true;
+    for (const Span* q = outs.begin(); q != &o; ++q)
+      if (o.n && q->n && overlap(o.p, o.n, q->p, q->n)) return true;
+  }
+  return false;
+}
 
 ekya_status check_workspace(const char* op, const void* ws, size_t bytes, size_t need) {
   if (bytes < need || (need && (!ws || !aligned(ws, 16))))
@@ -733,9 +749,12 @@ ekya_status ekya_op_groupnorm(int precision, const void* x, int N, long long HW,
       !std::isfinite(eps) || !gamma != !beta)
     return fail(nullptr, EKYA_ERR_INVALID_ARG, "invalid groupnorm arguments");
   if (N == 0) return EKYA_OK;
-  const size_t e = ekya::dtype_size(precision), bytes = (size_t)N * HW * C * e;
+  const size_t e = ekya::dtype_size(precision), bytes = (size_t)N * HW * C * e, stats = (size_t)N * groups * 4,
+               param = (size_t)C * 4;
   if (!x || !y || !mean || !rstd || !aligned(x, e) || !aligned(y, e) || !aligned(mean, 4) ||
-      !aligned(rstd, 4) || !aligned(gamma, 4) || !aligned(beta, 4) || partial_overlap(x, y, bytes))
+      !aligned(rstd, 4) || !aligned(gamma, 4) || !aligned(beta, 4) ||
+      outputs_overlap({{y, bytes, true}, {mean, stats}, {rstd, stats}},
+                      {{x, bytes, true}, {gamma, param}, {beta, param}}))
     return fail(nullptr, EKYA_ERR_INVALID_ARG, "groupnorm: null, misaligned or overlapping tensors");
   const size_t need = ekya::groupnorm_workspace_floats(precision, N, HW, C, groups, false) * sizeof(float);
   if (ekya_status s = check_workspace("groupnorm", workspace, workspace_bytes, need)) return s;
@@ -756,11 +775,13 @@ ekya_status ekya_op_groupnorm_backward(int precision, const void* dy, const void
   if (!groupnorm_sizes_ok(precision, N, HW, C, groups) || !valid_act(act) || !gamma != !beta ||
       !dgamma != !dbeta)
     return fail(nullptr, EKYA_ERR_INVALID_ARG, "invalid groupnorm_backward arguments");
-  const size_t e = ekya::dtype_size(precision), bytes = (size_t)N * HW * C * e;
+  const size_t e = ekya::dtype_size(precision), bytes = (size_t)N * HW * C * e, stats = (size_t)N * groups * 4,
+               param = (size_t)C * 4;
   if ((N > 0 && (!dy || !x || !mean || !rstd || !dx)) || !aligned(dy, e) || !aligned(x, e) ||
       !aligned(dx, e) || !aligned(gamma, 4) || !aligned(beta, 4) || !aligned(mean, 4) ||
       !aligned(rstd, 4) || !aligned(dgamma, 4) || !aligned(dbeta, 4) ||
-      partial_overlap(dx, dy, bytes) || partial_overlap(dx, x, bytes))
+      outputs_overlap({{dx, bytes, true}, {dgamma, param}, {dbeta, param}},
+                      {{dy, bytes, true}, {x, bytes, true}, {gamma, param}, {beta, param}, {mean, stats}, {rstd, stats}}))
     return fail(nullptr, EKYA_ERR_INVALID_ARG,
                 "groupnorm_backward: null, misaligned or overlapping tensors");
   const size_t need = ekya::groupnorm_workspace_floats(precision, N, HW, C, groups, true) * sizeof(float);
