@@ -770,13 +770,21 @@ def _ptr(t, shape, dtype, name: str):
     return t.data_ptr()
 
 
-def _groupnorm_dims(x):
+def _int_sizes(*sizes) -> None:
+    """Sizes that the C calls take as int: ctypes would cut off their upper bits."""
+    for n in sizes:
+        if n > 0x7FFFFFFF:
+            raise ValueError(f"a size of {n} is above 2^31 - 1")
+
+
+def _groupnorm_dims(x, groups: int):
     if x.dim() < 2:
         raise ValueError("group norm needs [N, ..., C]")
     shape = x.shape
     hw = 1
     for n in shape[1:-1]:
         hw *= n
+    _int_sizes(shape[0], shape[-1], groups)
     return shape[0], hw, shape[-1]
 
 
@@ -792,7 +800,7 @@ def ekya_op_groupnorm(x, groups: int, gamma=None, beta=None, eps: float = 1e-5,
     """(y, mean, rstd) of x [N, ..., C], channels last; y may be x."""
     torch = _torch()
     lib = load()
-    N, HW, C = _groupnorm_dims(x)
+    N, HW, C = _groupnorm_dims(x, groups)
     d = _on_current(x, gamma, beta, y)
     prec, dt, f32, shape = _precision(x), x.dtype, torch.float32, x.shape
     y = x.new_empty(shape) if y is None else y
@@ -811,7 +819,7 @@ def ekya_op_groupnorm_backward(dy, x, groups: int, gamma, beta, mean, rstd,
     """(dx, dgamma, dbeta); dx may be dy or x."""
     torch = _torch()
     lib = load()
-    N, HW, C = _groupnorm_dims(x)
+    N, HW, C = _groupnorm_dims(x, groups)
     d = _on_current(x, dy, gamma, beta, mean, rstd, dx)
     prec, dt, f32, shape = _precision(x), x.dtype, torch.float32, x.shape
     dx = x.new_empty(shape) if dx is None else dx
@@ -845,6 +853,7 @@ def _matmul_dims(x, w):
     if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
         raise ValueError(f"expected x [M, K] and w [N, K], got {tuple(x.shape)} and {tuple(w.shape)}")
     M, K = x.shape
+    _int_sizes(w.shape[0], K)
     return M, w.shape[0], K
 
 
