@@ -24,6 +24,7 @@
 
 #include "act.hpp"
 #include "kernels.hpp"
+#include "matmul_plan.hpp"
 
 namespace ekya {
 namespace {
@@ -521,78 +522,9 @@ bool unit16(const void* p, long long ld, int dt) {
   return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % dtype_vec(dt) == 0;
 }
 
-struct MmPlan {
-  int tile;            // outputs of a tile in either direction
-  int splits, stages;  // stages of a split (of a group of waves)
-  int groups;          // of waves in a block
-};
-// Which tile, and into how many parts the reduction is split.
-//
-// 256 x 256 (bf16 with DMA only) takes about 10 us and 1.58 us a stage for every
-// round of 256 tiles, one a CU; 128 x 128 about 5 us and 2.3 us and 0.46 us a
-// stage for every 256 tiles, two at a time on a CU, so that no round is waited
-// for.  Measured, 256 against 128: 8192^3 826 and 962 us, 4096^3 114 and 123,
-// 6272 x 2048 x 512 (200 tiles of 256) 23.2 and 25.2, 25088 x 1024 x 256 30.4 and
-// 31.1, 2048^3 (64 tiles of 256) 53.6 and 27.4.
-//
-// Up to 256 tiles of 128 with a reduction long enough for 512 parts of 8 stages:
-// two groups of waves a block, each with a part of the reduction, which overlap as
-// two blocks would and leave half the partial sums.  One group or 64 x 64 against
-// two groups: 2048^3 27.0 and 24.7 us, dw of 6272 x 512 x 2048 31.5 and 28.0, of
-// 25088 x 256 x 1024 30.7 and 27.1; 1500 x 4000 x 1500, whose 144 tiles leave CUs
-// idle, loses: 46.0 and 48.6.
-//
-// With less than 192 tiles of 128 most CUs hold one block or none: 64 x 64, and
-// the reduction split until 512 blocks run where a part is still 32 stages
-// long, else until 256 do (one a CU, three stages in flight).  128 against 64:
-// 1000^3 14.8 and 9.2 us, 512^3 10.3 and 6.0, but with 256 tiles of 128 2048^3
-// 27.4 and 28.0.  256 against 512 blocks: 128 x 2048 x 8192 (parts of 32 and 16
-// stages) 12.6 and 15.7, 256 x 1024 x 25088 (98 and 49) 40.6 and 33.4.  A part has
-// 16 stages at least (1024 x 512 x 4096 in parts of 32, 16 and 8: 21.6, 17.5 and
-// 19.2), 4 without DMA, whose stages take longer.
-//
-// fp32 is bound by the matrix cores with a block or two a CU already, so tile and
-// parts are those whose rounds come out even: a stage of a 128 x 128 tile takes
-// 2.3 us where a CU has one block and 2.0 for each where it has more, of 64 x 64
-// 1.0 and 0.6; adding up takes 4 us and the partial sums' traffic.  212 x 5079 x
-// 2955: 64 x 64 in two parts (188 tiles) 114 us, in four 94; 16384 x 512 x 300 dx:
-// 384 tiles of 128 72 us, 1280 of 64 54.
-MmPlan mm_fp32_plan(long long R, long long C, long long ns) {
-  MmPlan best{};
-  double least = 1e30;
-  for (int tile : {64, 128})
-    for (int s = 1; s <= 16 && s <= std::max(1LL, ns / 4); ++s) {
-      const long long stages = cdivl(ns, s), blocks = cdivl(cdivl(R, tile) * cdivl(C, tile) * s, 256);
-      const double stage = tile == 128 ? (blocks == 1 ? 2.3 : 2.0 * blocks) : blocks == 1 ? 1.0 : 0.6 * blocks;
-      const double us = stages * stage + (s > 1 ? 4 + s * (double)R * C * 8 / 4e6 : 0);
-      if (us < least) {
-        least = us;
-        best = {tile, (int)cdivl(ns, stages), (int)stages, 1};
-      }
-    }
-  return best;
-}
-MmPlan mm_plan(long long R, long long C, long long Tn, int dt, bool dma) {
-  const long long ns = std::max(1LL, cdivl(Tn, 8 * dtype_vec(dt)));
-  const long long t256 = cdivl(R, 256) * cdivl(C, 256), t128 = cdivl(R, 128) * cdivl(C, 128);
-  if (dt == DT_F32) return mm_fp32_plan(R, C, ns);
-  if (dma && t256 >= 192 &&
-      cdivl(t256, 256) * (10 + 1.58 * ns) <= 5 + t128 / 256. * (2.3 + 0.46 * ns))
-    return {256, 1, (int)ns, 1};
-  if (dma && std::min(R, C) >= 128 && t128 <= 256 && ns * t128 >= 512 * 8) {
-    const long long parts = 2 * (256 / t128), stages = cdivl(ns, parts);
-    return {128, (int)cdivl(ns, 2 * stages), (int)stages, 2};
-  }
-  if (t128 >= 192) return {128, 1, (int)ns, 1};
-  const long long t64 = std::max(1LL, cdivl(R, 64) * cdivl(C, 64));
-  const long long blocks = !dma || ns * t64 >= 512 * 32 ? 512 : 256;
-  const long long want = std::max(1LL, std::min(blocks / t64, ns / (dma ? 16 : 4)));
-  const int stages = (int)cdivl(ns, want);
-  return {64, (int)cdivl(ns, stages), stages, 1};
-}
 long long round4(long long n) { return (n + 3) & ~3LL; }
 size_t mm_part_floats(long long R, long long C, long long Tn, int dt, bool dma) {
-  const MmPlan p = mm_plan(R, C, Tn, dt, dma);
+  const MmPlan p = mm_plan(R, C, Tn, dt == DT_F32, dma);
   return p.splits > 1 ? (size_t)p.splits * C * round4(R) : 0;
 }
 
@@ -600,7 +532,7 @@ constexpr long long MM_TILES = 1 << 21;  // tiles of a launch
 
 template <typename T, typename OT, bool AOC, bool BOC, int ACT>
 hipError_t mm_run(MmArgs<T> a, bool dma, hipStream_t st) {
-  const MmPlan p = mm_plan(a.R, a.C, a.Tn, sizeof(T) == 2 ? DT_BF16 : DT_F32, dma);
+  const MmPlan p = mm_plan(a.R, a.C, a.Tn, sizeof(T) == 4, dma);
   a.splits = p.splits;
   a.Rp = round4(a.R);
   a.stages = p.stages;
@@ -677,14 +609,6 @@ struct MmMat {
   int padded(int dt) const { return (int)cdivl(cols, dtype_vec(dt)) * dtype_vec(dt); }
   size_t pack_floats(int dt) const { return ((size_t)rows * padded(dt) * dtype_size(dt) + 15) / 16 * 4; }
 };
-// Whether operands off 16 bytes are worth a padded copy.  Through registers a
-// bf16 product runs at about 300 TFLOP/s, with copies to LDS at 1100; a copied
-// element costs 4 bytes of traffic, so both directions of the result have to
-// be some hundreds long, and the product long enough for two more launches
-// (16384 x 2047 x 8192: 1812 us without).
-bool mm_pack(int dt, long long R, long long C, long long Tn) {
-  return dt == DT_BF16 && R * C >= 256 * (R + C) && (double)R * C * Tn >= 2e9;
-}
 template <typename T> hipError_t mm_copy(MmMat& m, float* ws, hipStream_t st) {
   const int dt = sizeof(T) == 2 ? DT_BF16 : DT_F32;
   const long long units = m.padded(dt) / Elt<T>::E, most = std::max(1LL, (1LL << 30) / units);
@@ -715,7 +639,7 @@ hipError_t mm_product(MmArgs<T> a, const MmMat& A, const MmMat& B, hipStream_t s
 
 size_t mm_forward_floats(const MatmulFwd& f) {
   const MmMat x{f.x, f.ldx, f.M, f.K}, w{f.w, f.ldw, f.N, f.K};
-  const bool copy = mm_pack(f.dt, f.N, f.M, f.K);
+  const bool copy = mm_pack(f.dt == DT_F32, f.N, f.M, f.K);
   size_t n = mm_part_floats(f.N, f.M, f.K, f.dt, copy || (x.units(f.dt) && w.units(f.dt)));
   if (copy)
     n += (x.units(f.dt) ? 0 : x.pack_floats(f.dt)) + (w.units(f.dt) ? 0 : w.pack_floats(f.dt));
@@ -725,7 +649,7 @@ size_t mm_forward_floats(const MatmulFwd& f) {
 template <typename T> hipError_t mm_forward(const MatmulFwd& f, float* ws, hipStream_t st) {
   const int dt = sizeof(T) == 2 ? DT_BF16 : DT_F32;
   MmMat x{f.x, f.ldx, f.M, f.K}, w{f.w, f.ldw, f.N, f.K};
-  if (mm_pack(dt, f.N, f.M, f.K))
+  if (mm_pack(dt == DT_F32, f.N, f.M, f.K))
     for (MmMat* m : {&x, &w})
       if (!m->units(dt)) {
         const size_t n = m->pack_floats(dt);
@@ -889,7 +813,7 @@ template <typename T> hipError_t mm_backward(const MatmulBwd& f, float* ws, hipS
     EKYA_HIP(unit ? (dz_run<T, Elt<T>::E>(a, f.act, f.db, st)) : (dz_run<T, 1>(a, f.act, f.db, st)));
   }
   MmMat g{dz, lddz, f.M, f.N};  // copied once for both products
-  const bool copy_dx = f.dx && mm_pack(dt, f.K, f.M, f.N), copy_dw = f.dw && mm_pack(dt, f.K, f.N, f.M);
+  const bool copy_dx = f.dx && mm_pack(dt == DT_F32, f.K, f.M, f.N), copy_dw = f.dw && mm_pack(dt == DT_F32, f.K, f.N, f.M);
   MmMat packed = g;
   if ((copy_dx || copy_dw) && f.M > 0 && !g.units(dt)) {
     const size_t n = g.pack_floats(dt);
@@ -941,7 +865,7 @@ size_t mm_backward_floats(const MatmulBwd& f) {
   const MmMat g{act ? f.dz : f.dy, act ? f.lddz : f.lddy, f.M, f.N}, x{f.x, f.ldx, f.M, f.K},
       w{f.w, f.ldw, f.N, f.K};
   const int dt = f.dt, E = dtype_vec(dt);
-  const bool copy_dx = f.dx && mm_pack(dt, f.K, f.M, f.N), copy_dw = f.dw && mm_pack(dt, f.K, f.N, f.M);
+  const bool copy_dx = f.dx && mm_pack(dt == DT_F32, f.K, f.M, f.N), copy_dw = f.dw && mm_pack(dt == DT_F32, f.K, f.N, f.M);
   size_t n = 0, db = 0;
   if (f.dx)
     n = mm_part_floats(f.K, f.M, f.N, dt, copy_dx || (w.units(dt) && g.units(dt))) + (copy_dx && !w.units(dt) ? w.pack_floats(dt) : 0);
