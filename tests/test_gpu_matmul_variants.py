@@ -59,3 +59,22 @@ def test_variant_gives_the_same_bits_again(v):
         assert all(torch.equal(a, b) for a, b in zip(captured, first))
     for g in got:
         assert all(torch.equal(a, b) for a, b in zip(g, first))
+
+
+@pytest.mark.parametrize("M,N,K", [(77, 45, 40), (130, 261, 24), (2000, 2001, 40), (3, 1001, 300)])
+@pytest.mark.parametrize("prec", ["f32", "bf16"])
+def test_residual_in_place_off_16_bytes(prec, M, N, K):
+    """Rows that no 16-byte unit divides: a lane's columns are read ahead of those it has finished."""
+    import torch
+    from paper_2012_10557_amd import binding
+    from tests.adapter_ref import strided
+    dtype = torch.float32 if prec == "f32" else torch.bfloat16
+    c = Case(M, N, K, dtype)
+    for act in ("none", "relu", "silu", "gelu"):
+        for first in (False, True):
+            y, _ = check_forward(c, act, True, True, first, False)
+            for ld, offset in ((N, 0), (N + 3, 1)):
+                res = strided(c.res, ld, offset)
+                got, _ = binding.ekya_op_matmul(c.x, c.w, c.bias, act=["none", "relu", "silu", "gelu"].index(act),
+                                                residual=res, residual_first=first, y=res)
+                assert got is res and torch.equal(got, y), (act, first, ld)
