@@ -38,30 +38,39 @@ struct MmPlan {
 // 19.2), 4 without DMA, whose stages take longer.
 //
 // fp32 is bound by the matrix cores with a block or two a CU already, so tile and
-// parts are those whose rounds come out even: a stage of a 128 x 128 tile takes
-// 2.3 us where a CU has one block and 2.0 for each where it has more, of 64 x 64
-// 1.0 and 0.6; adding up takes 4 us and the partial sums' traffic.  212 x 5079 x
-// 2955: 64 x 64 in two parts (188 tiles) 114 us, in four 94; 16384 x 512 x 300 dx:
-// 384 tiles of 128 72 us, 1280 of 64 54.
-inline MmPlan mm_fp32_plan(long long R, long long C, long long ns) {
+// parts are those with the least estimated time: a launch and what surrounds the
+// stages (4 us, 128 x 128 6), stages at what they take alone on a CU and with
+// other blocks beside them, adding up the parts (2 us and their traffic at 5.7
+// TB/s).  The constants are fitted to either tile and up to 16 parts of 70 sizes
+// (on those and 50 more the choice is 0.3% slower than the best of them on average,
+// 5% at most).  Without DMA a block alone on its CU waits for its loads.
+// 1000^3 in one part of 64 x 64 23.7 us, in two 27.3; 1500^3 78.6 and, in three, 73.2;
+// 1001 x 513 x 771 20.2 and, in two, 22.4; 212 x 5079 x 2955 in four parts of 64 x 64
+// 82.1, in ten of 128 x 128 89.7; 2048 x 520 x 2048 in 128 x 128 42.8, in 64 x 64 46.6;
+// 25088 x 256 x 256 dw in 8 parts 80.7, in 16 45.4; 7 x 320 x 976 dx in 7 parts of 5
+// stages 9.7, in 16 of 2 7.9.
+inline MmPlan mm_fp32_plan(long long R, long long C, long long ns, bool dma) {
   MmPlan best{};
   double least = 1e30;
-  for (int tile : {64, 128})
-    for (int s = 1; s <= 16 && s <= std::max(1LL, ns / 4); ++s) {
+  for (int tile : {64, 128}) {
+    const double alone = tile == 64 ? (dma ? 0.64 : 0.91) : dma ? 1.95 : 2.7;
+    const double beside = tile == 64 ? (dma ? 0.56 : 0.68) : dma ? 1.95 : 2.4;
+    for (int s = 1; s <= 16 && s <= ns; ++s) {
       const long long stages = mm_ceil(ns, s), blocks = mm_ceil(mm_ceil(R, tile) * mm_ceil(C, tile) * s, 256);
-      const double stage = tile == 128 ? (blocks == 1 ? 2.3 : 2.0 * blocks) : blocks == 1 ? 1.0 : 0.6 * blocks;
-      const double us = stages * stage + (s > 1 ? 4 + s * (double)R * C * 8 / 4e6 : 0);
+      const double us = (tile == 64 ? 4 : 6) + stages * (blocks == 1 ? alone : beside * blocks) +
+                        (s > 1 ? 2 + s * (double)R * C * 8 / 5.7e6 : 0);
       if (us < least) {
         least = us;
         best = {tile, (int)mm_ceil(ns, stages), (int)stages, 1};
       }
     }
+  }
   return best;
 }
 inline MmPlan mm_plan(long long R, long long C, long long Tn, bool fp32, bool dma) {
   const long long ns = std::max(1LL, mm_ceil(Tn, fp32 ? 32 : 64));
   const long long t256 = mm_ceil(R, 256) * mm_ceil(C, 256), t128 = mm_ceil(R, 128) * mm_ceil(C, 128);
-  if (fp32) return mm_fp32_plan(R, C, ns);
+  if (fp32) return mm_fp32_plan(R, C, ns, dma);
   if (dma && t256 >= 192 &&
       mm_ceil(t256, 256) * (10 + 1.58 * ns) <= 5 + t128 / 256. * (2.3 + 0.46 * ns))
     return {256, 1, (int)ns, 1};

@@ -30,9 +30,9 @@ VARIANTS = [
     ("128", "fp32", "forward", (2048, 2040, 520), True, (128, 1, 17, 1)),
     ("128", "fp32", "dx", (2048, 516, 2040), True, (128, 1, 17, 1)),
     ("128", "fp32", "dw", (515, 2048, 2040), True, (128, 1, 17, 1)),
-    ("128 without DMA", "fp32", "forward", (2048, 2037, 517), False, (128, 1, 17, 1)),
-    ("128 without DMA", "fp32", "dx", (2048, 517, 2037), False, (128, 1, 17, 1)),
-    ("128 without DMA", "fp32", "dw", (517, 2048, 2037), False, (128, 1, 17, 1)),
+    ("128 without DMA", "fp32", "forward", (4093, 2037, 517), False, (128, 1, 17, 1)),
+    ("128 without DMA", "fp32", "dx", (4093, 517, 2037), False, (128, 1, 17, 1)),
+    ("128 without DMA", "fp32", "dw", (517, 4093, 2037), False, (128, 1, 17, 1)),
 ]
 
 
