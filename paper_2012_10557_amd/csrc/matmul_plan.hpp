@@ -21,12 +21,17 @@ struct MmPlan {
 // 6272 x 2048 x 512 (200 tiles of 256) 23.2 and 25.2, 25088 x 1024 x 256 30.4 and
 // 31.1, 2048^3 (64 tiles of 256) 53.6 and 27.4.
 //
-// Up to 256 tiles of 128 with a reduction long enough for 512 parts of 8 stages:
-// two groups of waves a block, each with a part of the reduction, which overlap as
-// two blocks would and leave half the partial sums.  One group or 64 x 64 against
-// two groups: 2048^3 27.0 and 24.7 us, dw of 6272 x 512 x 2048 31.5 and 28.0, of
-// 25088 x 256 x 1024 30.7 and 27.1; 1500 x 4000 x 1500, whose 144 tiles leave CUs
-// idle, loses: 46.0 and 48.6.
+// Up to 256 tiles of 128 with a reduction long enough for 512 parts of 8 stages,
+// two ways of giving every CU two parts: two groups of waves a block, each with a
+// part of the reduction, whose sums meet in LDS, or two blocks of one group.  A
+// stage takes 1.42 us in the two groups and 1.10 in the two blocks, which in turn
+// leave twice the partial sums and fill CUs that 256 / tiles rounded down leaves
+// idle.  Two groups against two blocks: 2040^2 x 2264 33.7 and 39.9 us, 760^2 x 7448
+// 28.0 and 29.5, 500^2 x 35992 39.6 and 41.4, but 1500^2 x 3992 (144 tiles) 47.8 and
+// 38.6, 1280 x 1150 x 12760 83.5 and 62.9, 896 x 900 x 18008 60.6 and 53.8.  One
+// group unsplit or 64 x 64 against the better of the two: 2040^2 x 2264 36.8 and 33.7,
+// 1500^2 x 3992 52.0 and 38.6, 760^2 x 7448 31.6 and 28.0; dw of 6272 x 512 x 2048 31.5 and
+// 28.0, of 25088 x 256 x 1024 30.7 and 27.1.
 //
 // With less than 192 tiles of 128 most CUs hold one block or none: 64 x 64, and
 // the reduction split until 512 blocks run where a part is still 32 stages
@@ -75,8 +80,12 @@ inline MmPlan mm_plan(long long R, long long C, long long Tn, bool fp32, bool dm
       mm_ceil(t256, 256) * (10 + 1.58 * ns) <= 5 + t128 / 256. * (2.3 + 0.46 * ns))
     return {256, 1, (int)ns, 1};
   if (dma && std::min(R, C) >= 128 && t128 <= 256 && ns * t128 >= 512 * 8) {
-    const long long parts = 2 * (256 / t128), stages = mm_ceil(ns, parts);
-    return {128, (int)mm_ceil(ns, 2 * stages), (int)stages, 2};
+    const long long parts = 256 / t128, blocks = 512 / t128;  // of the reduction, for two groups and for one
+    const long long two = mm_ceil(ns, 2 * parts), one = mm_ceil(ns, blocks);
+    const double adding = (double)R * C * 8 / 5.7e6;  // a part's sums, written and read
+    if (1.42 * two + (parts > 1 ? 2 + parts * adding : 0) <= 1.10 * one + 2 + blocks * adding)
+      return {128, (int)mm_ceil(ns, 2 * two), (int)two, 2};
+    return {128, (int)mm_ceil(ns, one), (int)one, 1};
   }
   if (t128 >= 192) return {128, 1, (int)ns, 1};
   const long long t64 = std::max(1LL, mm_ceil(R, 64) * mm_ceil(C, 64));

@@ -20,7 +20,10 @@ VARIANTS = [
     ("two groups, an idle one", "bf16", "forward", (500, 504, 16400), True, (128, 15, 9, 2)),
     ("two groups, an idle one", "bf16", "dx", (500, 16400, 504), True, (128, 15, 9, 2)),
     ("two groups, an idle one", "bf16", "dw", (16395, 496, 504), True, (128, 15, 9, 2)),
-    # 128 x 128 with one group
+    # 128 x 128 with one group: parts of the reduction, the last a stage shorter, or the whole of it
+    ("128, splits", "bf16", "forward", (1500, 1496, 3944), True, (128, 3, 21, 1)),
+    ("128, splits", "bf16", "dx", (1500, 3944, 1496), True, (128, 3, 21, 1)),
+    ("128, splits", "bf16", "dw", (3931, 1504, 1496), True, (128, 3, 21, 1)),
     ("128", "bf16", "forward", (2000, 1992, 936), True, (128, 1, 15, 1)),
     ("128", "bf16", "dx", (2000, 936, 1992), True, (128, 1, 15, 1)),
     ("128", "bf16", "dw", (931, 2000, 1992), True, (128, 1, 15, 1)),
