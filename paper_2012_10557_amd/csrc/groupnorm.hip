@@ -775,19 +775,32 @@ hipError_t gn_fused_samples(const GnArgs& a, const GnFuse& f, F&& go) {
   });
 }
 
+// Units of a thread: 64 of its 128 registers (1024 threads a block) hold them in
+// fp32 and in the backward pass, whose units are pairs; bf16 forward stays at the
+// same 16, with which two blocks fit a CU.  A call takes the smallest kernel that
+// holds its units, since a short sample is bound by fetching code (128 x 784 x 128
+// backward with 8 units 28.1 us, with 16 30.2; 4096 pixels of 64 channels with 16
+// 37.4 forward and 68.4 backward, in several launches 49.3 and 76.1).
+template <typename T, bool BACK> constexpr int GN_UNITS = BACK && sizeof(T) == 4 ? 8 : 16;
+template <int MOST, typename F> auto gn_units(int need, F&& f) {
+  if (need <= 3) return f(std::integral_constant<int, 3>{});
+  if constexpr (MOST > 8)
+    if (need > 8) return f(std::integral_constant<int, MOST>{});
+  return f(std::integral_constant<int, 8>{});
+}
+
 template <typename T, int E> hipError_t gn_forward(GnArgs a, int act, hipStream_t st) {
   if constexpr (E > 1) {
-    constexpr int EU = 4, R = 13;
+    constexpr int EU = 4, R = GN_UNITS<T, false>;
     GnFuse f;
     int threads;
     if (gn_fuse(a, EU, sizeof(T), R, f, threads))
       return gn_fused_samples<T, EU>(a, f, [&](const GnArgs& b, dim3 grid) {
         return act_dispatch(act, [&](auto k) {
-          if (f.need <= 3)
-            hipLaunchKernelGGL((gn_fused_kernel<T, EU, k.value, 3>), grid, dim3(threads), 0, st, b, f);
-          else
-            hipLaunchKernelGGL((gn_fused_kernel<T, EU, k.value, R>), grid, dim3(threads), 0, st, b, f);
-          return hipGetLastError();
+          return gn_units<R>(f.need, [&](auto r) {
+            hipLaunchKernelGGL((gn_fused_kernel<T, EU, k.value, r.value>), grid, dim3(threads), 0, st, b, f);
+            return hipGetLastError();
+          });
         });
       });
   }
@@ -827,17 +840,16 @@ hipError_t gn_param(const GnArgs& a, const float* src, long long rows, GnColumns
 template <typename T, int E> hipError_t gn_backward(GnArgs a, int act, hipStream_t st) {
   if constexpr (E > 1) {
     // 8-byte units in bf16: a unit's constants and sums take half the registers
-    constexpr int EU = 4, R = sizeof(T) == 2 ? 13 : 7;
+    constexpr int EU = 4, R = GN_UNITS<T, true>;
     GnFuse f;
     int threads;
     if (gn_fuse(a, EU, sizeof(T), R, f, threads)) {
       EKYA_HIP((gn_fused_samples<T, EU>(a, f, [&](const GnArgs& b, dim3 grid) {
         return act_dispatch(act, [&](auto k) {
-          if (f.need <= 3)
-            hipLaunchKernelGGL((gn_fused_bwd_kernel<T, EU, k.value, 3>), grid, dim3(threads), 0, st, b, f);
-          else
-            hipLaunchKernelGGL((gn_fused_bwd_kernel<T, EU, k.value, R>), grid, dim3(threads), 0, st, b, f);
-          return hipGetLastError();
+          return gn_units<R>(f.need, [&](auto r) {
+            hipLaunchKernelGGL((gn_fused_bwd_kernel<T, EU, k.value, r.value>), grid, dim3(threads), 0, st, b, f);
+            return hipGetLastError();
+          });
         });
       })));
       if (!a.dgamma) return hipSuccess;
