@@ -1747,9 +1747,10 @@ ekya_status run_profile(Ctx& c, const float* weights, const ekya_profile_cfg* cf
   // A classifier-only epoch takes tens of microseconds, and a process's first
   // launch of its kernels, on the host and cold on the GPU, adds to it: 77 to 106
   // us (16 processes), after a step that is not timed 74 to 81.  That step comes
-  // before the first such candidate, whose state is then set up anew.
+  // before the first such candidate, whose state is then set up anew (not where
+  // launches are being timed one by one: it would be among them).
   int cold = -1;
-  for (int i = n_cfgs - 1; i >= 0 && !concurrent; --i)
+  for (int i = n_cfgs - 1; i >= 0 && !concurrent && !c.timing; --i)
     if (jobs[i].lowest == 5 && jobs[i].n_s > 0) cold = i;
   auto first_use = [](TrainJob& j) -> hipError_t {
     EKYA_HIP(job_setup(j));
