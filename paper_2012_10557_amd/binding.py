@@ -923,9 +923,10 @@ class Adamw:
     captured step reads and writes the tensors it was captured with: keep the
     handle, and those gradients, as long as its graph is replayed."""
 
-    def __init__(self, handle, tensors, grads):
+    def __init__(self, handle, tensors, shapes, grads):
         self.handle = handle
-        self.tensors = tensors  # [w, m, v, scale, low] of each
+        self.tensors = tensors  # the memory of each one's w, m, v, scale and low
+        self.shapes = shapes
         self.grads = grads      # those that the next step takes
         self.device = grads[0].device if grads else None
         self._destroy = load().ekya_adamw_destroy
@@ -949,11 +950,12 @@ def ekya_adamw_create(tensors: Sequence[dict], state_bits: int = 32) -> Adamw:
     mt, vt = (torch.float8_e4m3fn, torch.float8_e5m2) if state_bits == 8 else (f32, f32)
     arr = (AdamwTensor * max(1, len(tensors)))()
     gtype = tensors[0]["g"].dtype if tensors else f32
-    kept, grads = [], []
+    kept, shapes, grads = [], [], []
     for i, t in enumerate(tensors):
         w, g, m, v, scale, low = t["w"], t["g"], t["m"], t["v"], t.get("scale"), t.get("low")
-        # aliases: the memory stays even where a tensor is given another (t.data = ..)
-        kept.append([k if k is None else k.detach() for k in (w, m, v, scale, low)])
+        # the memory itself: a tensor may be given another (t.data = ..)
+        kept.append([k.untyped_storage() for k in (w, m, v, scale, low) if k is not None])
+        shapes.append(w.shape)
         grads.append(g)
         _on_current(w, g, m, v, scale, low)
         shape, n = w.shape, w.numel()
@@ -963,7 +965,7 @@ def ekya_adamw_create(tensors: Sequence[dict], state_bits: int = 32) -> Adamw:
     h = ctypes.c_void_p()
     prec = EKYA_FP32 if gtype == f32 else EKYA_BF16 if gtype == bf16 else -1
     _op(load().ekya_adamw_create(ctypes.byref(h), arr, len(tensors), prec, state_bits))
-    return Adamw(h, kept, grads)
+    return Adamw(h, kept, shapes, grads)
 
 
 def ekya_adamw_destroy(opt: Adamw) -> None:
@@ -973,12 +975,12 @@ def ekya_adamw_destroy(opt: Adamw) -> None:
 def ekya_adamw_set_grads(opt: Adamw, grads: Sequence) -> None:
     """New gradient tensors of the same shapes and type; later steps take them, and the former
     ones are let go."""
-    if len(grads) != len(opt.tensors):
+    if len(grads) != len(opt.shapes):
         raise ValueError("one gradient per tensor")
     arr = (_P * max(1, len(grads)))()
-    for i, (g, t) in enumerate(zip(grads, opt.tensors)):
-        _on_current(t[0], g)
-        arr[i] = _ptr(g, t[0].shape, opt.grads[0].dtype, "gradient")
+    for i, (g, old, shape) in enumerate(zip(grads, opt.grads, opt.shapes)):
+        _on_current(old, g)
+        arr[i] = _ptr(g, shape, old.dtype, "gradient")
     _op(load().ekya_adamw_set_grads(opt.handle, arr, len(grads)))
     opt.grads = list(grads)
 
