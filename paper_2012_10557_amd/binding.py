@@ -770,11 +770,11 @@ def _ptr(t, shape, dtype, name: str):
     return t.data_ptr()
 
 
-def _int_sizes(*sizes) -> None:
-    """Sizes that the C calls take as int: ctypes would cut off their upper bits."""
-    for n in sizes:
-        if n > 0x7FFFFFFF:
-            raise ValueError(f"a size of {n} is above 2^31 - 1")
+_INT_MAX = 0x7FFFFFFF  # of the sizes that C takes as int: ctypes would cut off what is above
+
+
+def _too_large(*sizes):
+    return ValueError(f"a size of {max(sizes)} is above 2^31 - 1")
 
 
 def _groupnorm_dims(x, groups: int):
@@ -784,8 +784,10 @@ def _groupnorm_dims(x, groups: int):
     hw = 1
     for n in shape[1:-1]:
         hw *= n
-    _int_sizes(shape[0], shape[-1], groups)
-    return shape[0], hw, shape[-1]
+    N, C = shape[0], shape[-1]
+    if N > _INT_MAX or C > _INT_MAX or groups > _INT_MAX:
+        raise _too_large(N, C, groups)
+    return N, hw, C
 
 
 @functools.lru_cache(maxsize=256)
@@ -852,9 +854,10 @@ def _matrix(t, rows: int, cols: int, dtype, name: str):
 def _matmul_dims(x, w):
     if x.dim() != 2 or w.dim() != 2 or x.shape[1] != w.shape[1]:
         raise ValueError(f"expected x [M, K] and w [N, K], got {tuple(x.shape)} and {tuple(w.shape)}")
-    M, K = x.shape
-    _int_sizes(w.shape[0], K)
-    return M, w.shape[0], K
+    (M, K), N = x.shape, w.shape[0]
+    if N > _INT_MAX or K > _INT_MAX:
+        raise _too_large(N, K)
+    return M, N, K
 
 
 def ekya_op_matmul(x, w, bias=None, act: int = EKYA_ACT_NONE, residual=None,
