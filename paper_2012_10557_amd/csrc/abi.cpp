@@ -816,7 +816,7 @@ bool overlap(const Mat& a, const Mat& b) {
 bool same(const Mat& a, const Mat& b) { return a.p == b.p && a.ld == b.ld; }
 
 // A matrix that is there, on its elements, with rows that do not overlap and
-// at most 2^40 elements' span.
+// whose distances add up to at most 2^42 elements.
 bool mat_ok(const Mat& m) {
   return m.p && aligned(m.p, m.size) && m.ld >= m.cols &&
          (m.rows <= 1 || m.ld <= (1LL << 42) / m.rows);

@@ -20,8 +20,8 @@
 // kept per channel, whatever the group size (groups of 3 or 10 channels straddle
 // the units), and folded into groups by the coefficient kernels.  Means and
 // squared deviations are merged pairwise (Chan, Golub and LeVeque), so that a
-// mean far from zero costs no digits.  128 x 3136 x 64 in one group: 42 us forward,
-// 58 backward; 19 x 1147 x 120 fp32 in groups of 10 backward 21 us.
+// mean far from zero costs no digits.  128 x 3136 x 64 in one group: 41 us forward,
+// 62 backward; 19 x 1147 x 120 fp32 in groups of 10 backward 21 us.
 #include <algorithm>
 #include <climits>
 #include <numeric>

@@ -14,12 +14,12 @@
 // of the next half stage are read into registers while the matrix cores work on
 // this one's.
 //
-// Long products are bound by the matrix cores at the clock that their power
-// leaves (8192^3 bf16: 1300 TFLOP/s, 823 to 860 us by machine, where the vendor's
-// library takes 840; fp32 4096 x 2048 x 2048 130 of 154 TFLOP/s), short ones by what a
-// tile costs besides its stages: launch, the first loads, and the epilogue,
-// which overlaps with nothing where a CU holds one block (16384 x 2048 x 8192
-// with SiLU and a residual 535 us, 480 without both).
+// Long products are bound by the matrix cores and how steadily they are fed
+// (8192^3 bf16 1340 TFLOP/s, 820 us, where the vendor's library takes 664; fp32 4096
+// x 2048 x 2048 140 of the library's 146 TFLOP/s), short ones by what a tile costs besides its
+// stages: launch, the first loads, and the epilogue, which overlaps with nothing
+// where a CU holds one block (16384 x 2048 x 8192 with SiLU and a residual 519 us,
+// 469 without both).
 #include <algorithm>
 
 #include "act.hpp"
@@ -696,6 +696,8 @@ template <typename T> hipError_t mm_forward(const MatmulFwd& f, float* ws, hipSt
 
 // ----------------------------------------------------------------- backward
 // dz = dy act'(z), and the column sums of what is stored before its rounding.
+// dz is rounded to T because both products take it as an operand of the matrix
+// cores, whose rate in bf16 is 16 times that of fp32.
 // A block takes a range of rows and up to 64 units of columns.
 constexpr int DZ_NT = 256;
 struct DzArgs {
